@@ -58,6 +58,8 @@ extern "C" {
 #define CHAM_E_BAD_FLAG     (-8)   /* unknown bits in flags / unknown init_mode */
 #define CHAM_E_NOMEM        (-9)   /* host memory for the call's small tables could not be had */
 #define CHAM_E_TOO_LARGE    (-10)  /* cham_kmeans_sweep_static: the input needs more scratch than the static buffer holds */
+#define CHAM_E_BAD_TYPE     (-11)  /* a CHAM_TYPE_* that the entry point does not take */
+#define CHAM_E_BAD_COEF     (-12)  /* a coefficient that is not finite or outside its range */
 
 /* values of out_flag (cham_synthesize) */
 #define CHAM_OUT_EMPTY   0   /* cluster has no member (or index >= chosen k) */
@@ -321,7 +323,7 @@ int32_t cham_synthesize_table(const uint8_t *X, int64_t ld, int32_t d,
  * Configuration updater of the exploration step that feeds the sampling step (Sec. 3.2, the
  * action figure: the agent emits increment / decrement / stay per knob, the updater applies it;
  * hyper-parameter table: 128 episodes of up to 500 steps).  The policy network is not part of this
- * library: the actions are an input.
+ * library: the actions are an input (its update: cham_policy_loss and what follows it).
  *   theta   DEVICE uint8 [B][d]           configurations, updated in place through n_steps steps:
  *                                         theta <- clip(theta + a, 0, card - 1) per knob
  *   actions DEVICE int8 [n_steps][B][d]   each -1, 0 or +1
@@ -340,6 +342,147 @@ int32_t cham_update_configs(uint8_t *theta, const int8_t *actions, int64_t B, in
                             const uint16_t *cards, uint64_t salt, uint64_t *seen_table, int64_t slots,
                             uint8_t *unique_rows, int64_t capacity, int32_t *n_unique, int32_t *overflow,
                             void *stream);
+
+/*
+ * The agent's update (Sec. 3.4: the exploration agent is an actor-critic trained with clipped policy updates; table of
+ * its hyper-parameters: clip 0.3, entropy 0.1, value 1.0, discount 0.9, GAE 0.99, 3 epochs).  The networks themselves
+ * are the caller's: logits and values come in, gradients with respect to them go out, and the gradients of the
+ * networks' own tensors come back to be clipped by their global norm.  The decisions are those whose actions
+ * cham_update_configs applies; a policy with one head of many choices (a language model's tokens) is the case heads = 1.
+ *
+ * Layout.  R decisions with G heads of V choices each: logit v of head g of decision r stands at
+ * logits[r*ld_r + g*ld_g + v] (strides in items).  Trajectories of n_steps x B x d knobs are R = n_steps * B decisions
+ * of G = d heads with V = 3 directions; the action -1, 0, +1 is choice 0, 1, 2 with first_action = -1.  Heads do not
+ * overlap, in either order of the strides (a stride that is never taken, R = 1 or G = 1, is not looked at).
+ *
+ * CHAM_TYPE_*: the type of logits, gradients, rewards and values (bf16, f16: 16-bit floats), or of actions.
+ */
+#define CHAM_TYPE_F32  0
+#define CHAM_TYPE_BF16 1
+#define CHAM_TYPE_F16  2
+#define CHAM_TYPE_I8   16
+#define CHAM_TYPE_I32  17
+#define CHAM_TYPE_I64  18
+
+/* Bytes of DEVICE workspace of cham_policy_logp (want_grad = 0) and cham_policy_loss (0 without grad_logits, 1 with),
+ * or a negative error. */
+int64_t cham_policy_workspace_bytes(int64_t R, int32_t G, int32_t V, int32_t type, int32_t want_grad);
+
+/*
+ * Log-probability of the actions taken and the policy's entropy, per decision (the old and the reference policy's side
+ * of cham_policy_loss, or an evaluation):
+ *   logp[r]    = sum_g ( x[r,g,a] - log sum_v exp x[r,g,v] )          a = actions[r*G + g] - first_action
+ *   entropy[r] = sum_g ( - sum_v p[r,g,v] log p[r,g,v] )
+ *   logits  DEVICE [R][G][V] of `type` (f32, bf16, f16), aligned to its items
+ *   actions DEVICE [R][G] dense, of action_type (i8, i32, i64)
+ *   weights DEVICE float [R] or NULL: a decision of weight 0 is left out: nothing of it is read, its outputs are 0
+ *   logp, entropy DEVICE float [R]; entropy may be NULL
+ * A masked choice has the logit -inf (or its type's lowest value): probability 0, nothing added to the entropy.  A head
+ * whose choices are all -inf, or whose action is below first_action (a padded knob), is left out of its decision; a
+ * decision with no head left is left out.  An action at or above first_action + V, and a NaN or +inf among a head's logits,
+ * give NaN.  Exponentials and their sums are taken in fp32, sums over heads in double.
+ * Errors: CHAM_E_NULL, CHAM_E_BAD_DIM (R < 0, G outside [1, 65536], V outside [1, 2^24], more than 2^40 heads in all,
+ * overlapping strides, misaligned pointers), CHAM_E_BAD_TYPE, CHAM_E_WORKSPACE.  R = 0 is no error.
+ */
+int32_t cham_policy_logp(const void *logits, int32_t type, int64_t R, int32_t G, int32_t V, int64_t ld_r, int64_t ld_g,
+                         const void *actions, int32_t action_type, int64_t first_action, const float *weights,
+                         float *logp, float *entropy, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Coefficients of cham_policy_loss, all finite and not negative. */
+typedef struct cham_policy_coef {
+    double clip_low, clip_high;   /* the ratio counts within [1 - clip_low, 1 + clip_high] */
+    double value;                 /* factor of the value term */
+    double entropy;               /* factor of the entropy (subtracted: a bonus) */
+    double kl;                    /* factor of the divergence from the reference policy */
+    double value_clip;            /* how far a value counts from old_values (not looked at without them) */
+} cham_policy_coef;
+
+/* terms of cham_policy_loss: sums over the decisions, each times its weight */
+#define CHAM_TERM_TOTAL   0   /* policy + value * VALUE - entropy * ENTROPY + kl * KL */
+#define CHAM_TERM_POLICY  1   /* -min(ratio A, clip(ratio) A),  ratio = exp(logp - old_logp) */
+#define CHAM_TERM_VALUE   2   /* max((v - ret)^2, (old_v + clip(v - old_v) - ret)^2) / 2; without old_values (v - ret)^2 / 2 */
+#define CHAM_TERM_ENTROPY 3
+#define CHAM_TERM_KL      4   /* e^d - d - 1,  d = ref_logp - logp: not negative, its mean over the policy's actions the divergence */
+#define CHAM_TERM_CLIPPED 5   /* 1 where the clip decides (ratio A above clip(ratio) A) */
+#define CHAM_TERMS        6
+
+/*
+ * Clipped policy loss with its gradients.  Arguments up to weights, and the decisions left out, as cham_policy_logp;
+ *   weights NULL: 1 / R each.  A weight carries the mean over decisions (1 / how many count), a padded decision's 0, and
+ *           the scale of a loss whose gradients are f16
+ *   old_logp, advantages DEVICE float [R]
+ *   ref_logp DEVICE float [R] or NULL (only with coef->kl = 0): log-probabilities under a reference policy
+ *   values, returns DEVICE float [R], both or neither (neither only with coef->value = 0); old_values DEVICE float [R] or NULL
+ *   coef    HOST
+ *   terms   DEVICE float [CHAM_TERMS], each summed in double in a fixed order
+ *   logp, entropy DEVICE float [R], either may be NULL
+ *   grad_logits DEVICE, of the logits' type, at strides gld_r, gld_g: the gradient of the total, every item written (zeros for
+ *           what is left out; other memory between strides is left as it was).  NULL: forward only.  It may be the
+ *           logits themselves (same pointer and strides: in place); any other overlap is refused
+ *   grad_values DEVICE float [R] or NULL
+ * The gradient of a minimum or maximum is that of the unclipped side where both are equal.  A term whose coefficient is
+ * 0 adds nothing to the total or the gradients, whatever its value.  Per-decision arithmetic is in double.
+ * Errors: as cham_policy_logp, CHAM_E_BAD_COEF.
+ */
+int32_t cham_policy_loss(const void *logits, int32_t type, int64_t R, int32_t G, int32_t V, int64_t ld_r, int64_t ld_g,
+                         const void *actions, int32_t action_type, int64_t first_action, const float *weights,
+                         const float *old_logp, const float *advantages, const float *ref_logp,
+                         const float *values, const float *old_values, const float *returns,
+                         const cham_policy_coef *coef, float *terms, float *logp, float *entropy,
+                         void *grad_logits, int64_t gld_r, int64_t gld_g, float *grad_values,
+                         void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of DEVICE workspace of cham_gae, or a negative error. */
+int64_t cham_gae_workspace_bytes(int64_t B, int64_t S);
+
+/*
+ * Advantages (generalised advantage estimation) and returns of B trajectories of up to S steps:
+ *   delta_t = r_t + gamma n_t V_{t+1} - V_t,  A_t = delta_t + gamma lambda n_t A_{t+1},  ret_t = A_t + V_t,
+ * n_t = 0 where done_t is set and 1 elsewhere, V behind the last step = bootstrap, A behind it = 0.
+ *   rewards, values DEVICE of `type` (f32, bf16, f16): step s of trajectory b at [b*ld_b + s*ld_s], any strides >= 0
+ *   dones     DEVICE uint8, same addressing, or NULL (no episode ends inside)
+ *   bootstrap DEVICE float [B] or NULL (zeros): value of the state behind the last step
+ *   lengths   DEVICE int32 [B] or NULL (S each): steps of every trajectory, taken into [0, S]; outputs at and behind a
+ *             length are left as they were
+ *   advantages, returns DEVICE float at strides o_ldb, o_lds, which do not overlap; returns may be NULL; no input may share
+ *             memory with an output
+ * The recurrence is evaluated in double and rounded once.  It is joined from runs of steps in an order that depends on B, S
+ * and the strides alone.
+ * Errors: CHAM_E_NULL, CHAM_E_BAD_DIM (B < 0, S outside [0, 2^31), B * S above 2^40, negative or overlapping strides, misaligned
+ * pointers), CHAM_E_BAD_TYPE, CHAM_E_BAD_COEF (gamma or lambda outside [0, 1]), CHAM_E_WORKSPACE.
+ */
+int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_t r_ldb, int64_t r_lds,
+                 const void *values, int64_t v_ldb, int64_t v_lds, const uint8_t *dones, int64_t d_ldb, int64_t d_lds,
+                 const float *bootstrap, const int32_t *lengths, double gamma, double lambda,
+                 float *advantages, float *returns, int64_t o_ldb, int64_t o_lds,
+                 void *workspace, int64_t workspace_bytes, void *stream);
+
+/* flag of cham_clip_grads: *norm is an input */
+#define CHAM_F_NORM_GIVEN 32
+
+/* Bytes of DEVICE workspace of cham_grad_norm and cham_clip_grads, or a negative error. */
+int64_t cham_grad_workspace_bytes(const int64_t *numels, const int32_t *types, int32_t n);
+
+/*
+ * Norm of all gradients together, and clipping by it.
+ *   grads  HOST array of n DEVICE pointers, numels HOST int64 (0 allowed: that pointer is not looked at), types HOST
+ *          CHAM_TYPE_F32 / BF16 / F16 each; every tensor contiguous, aligned to its items
+ *   norm   DEVICE double: sqrt of the sum of all squares, squares and sums in double (no square overflows or vanishes)
+ * cham_clip_grads then scales every gradient by max_norm / (norm + 1e-6) unless norm + 1e-6 <= max_norm; gradients are
+ * multiplied in fp32 and rounded once.  A NaN norm makes every gradient NaN, an infinite one makes finite gradients 0.
+ *   outs   HOST array of n DEVICE pointers: where the clipped gradients go (an unclipped copy where nothing is clipped);
+ *          NULL: in place (not written at all where nothing is clipped).  outs[i] may be grads[i]; other overlaps are the
+ *          caller's to avoid
+ *   flags  CHAM_F_NORM_GIVEN: *norm is read instead of computed (the norm over several processes' parts, say)
+ * n = 0 gives the norm 0.  Results do not depend on the order in which workgroups run.
+ * Errors: CHAM_E_NULL, CHAM_E_BAD_DIM (n < 0, a negative or too large count (2^40 in all), misaligned pointers),
+ * CHAM_E_BAD_TYPE, CHAM_E_BAD_COEF (max_norm negative or NaN), CHAM_E_BAD_FLAG, CHAM_E_WORKSPACE.
+ */
+int32_t cham_grad_norm(const void *const *grads, const int64_t *numels, const int32_t *types, int32_t n, double *norm,
+                       void *workspace, int64_t workspace_bytes, void *stream);
+int32_t cham_clip_grads(const void *const *grads, void *const *outs, const int64_t *numels, const int32_t *types, int32_t n,
+                        double max_norm, double *norm, void *workspace, int64_t workspace_bytes, int32_t flags,
+                        void *stream);
 
 /*
  * Configuration hash used for the visited set: 64-bit FNV-1a over the d knob values, the

@@ -17,6 +17,9 @@ LIB_PATH = os.path.join(_HERE, "libcham.so")
 
 F_FORCE_EXACT, F_STREAMING, F_RESIDENT, F_NO_MFMA = 1, 2, 4, 8
 F_VALUES_BELOW_2048 = 16
+F_NORM_GIVEN = 32
+TYPE_F32, TYPE_BF16, TYPE_F16, TYPE_I8, TYPE_I32, TYPE_I64 = 0, 1, 2, 16, 17, 18
+TERMS = ("total", "policy", "value", "entropy", "kl", "clipped")
 OUT_EMPTY, OUT_KEPT, OUT_SYNTH, OUT_DROPPED = 0, 1, 2, 3
 
 EXPORTS = [
@@ -31,11 +34,17 @@ EXPORTS = [
     "cham_kmeans_sweep_knee_u16", "cham_snap_workspace_bytes_u16", "cham_snap_centroids_u16",
     "cham_synth_workspace_bytes_u16", "cham_synthesize_u16", "cham_synthesize_table_u16",
     "cham_visited_table_insert_configs_u16", "cham_hash_config_u16", "cham_hash_rows_u16",
+    "cham_policy_workspace_bytes", "cham_policy_logp", "cham_policy_loss", "cham_gae_workspace_bytes", "cham_gae",
+    "cham_grad_workspace_bytes", "cham_grad_norm", "cham_clip_grads",
 ]
 
 
 class ChamError(RuntimeError):
     pass
+
+
+class _PolicyCoef(C.Structure):
+    _fields_ = [(name, C.c_double) for name in ("clip_low", "clip_high", "value", "entropy", "kl", "value_clip")]
 
 
 _lib = None
@@ -115,6 +124,24 @@ def load() -> C.CDLL:
         lib.cham_hash_config.argtypes = [vp, i32, u64]
         lib.cham_hash_rows.restype = i32
         lib.cham_hash_rows.argtypes = [vp, i64, i32, vp, u64, vp, vp]
+        lib.cham_policy_workspace_bytes.restype = i64
+        lib.cham_policy_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+        lib.cham_policy_logp.restype = i32
+        lib.cham_policy_logp.argtypes = [vp, i32, i64, i32, i32, i64, i64, vp, i32, i64, vp, vp, vp, vp, i64, vp]
+        lib.cham_policy_loss.restype = i32
+        lib.cham_policy_loss.argtypes = [vp, i32, i64, i32, i32, i64, i64, vp, i32, i64, vp, vp, vp, vp, vp, vp, vp,
+                                         C.POINTER(_PolicyCoef), vp, vp, vp, vp, i64, i64, vp, vp, i64, vp]
+        lib.cham_gae_workspace_bytes.restype = i64
+        lib.cham_gae_workspace_bytes.argtypes = [i64, i64]
+        lib.cham_gae.restype = i32
+        lib.cham_gae.argtypes = [i32, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, f64, f64, vp, vp, i64, i64,
+                                 vp, i64, vp]
+        lib.cham_grad_workspace_bytes.restype = i64
+        lib.cham_grad_workspace_bytes.argtypes = [vp, vp, i32]
+        lib.cham_grad_norm.restype = i32
+        lib.cham_grad_norm.argtypes = [vp, vp, vp, i32, vp, vp, i64, vp]
+        lib.cham_clip_grads.restype = i32
+        lib.cham_clip_grads.argtypes = [vp, vp, vp, vp, i32, f64, vp, vp, i64, i32, vp]
         # the entry points for two-byte knobs take the same argument lists
         for name in EXPORTS:
             if name.endswith("_u16"):
@@ -532,6 +559,225 @@ def cham_update_configs(theta, actions, cards, salt: int = 0, seen_table=None, u
                                       C.c_int64(0 if unique_rows is None else unique_rows.shape[0]), _dp(n_unique),
                                       _dp(overflow), _stream()))
     return theta
+
+
+_FLOAT_TYPES = {"torch.float32": TYPE_F32, "torch.bfloat16": TYPE_BF16, "torch.float16": TYPE_F16}
+_ACTION_TYPES = {"torch.int8": TYPE_I8, "torch.int32": TYPE_I32, "torch.int64": TYPE_I64}
+
+
+def _type_of(t, types, what: str) -> int:
+    code = types.get(str(t.dtype))
+    if code is None:
+        raise ChamError(f"{what}: {t.dtype} is not one of {', '.join(types)}")
+    return code
+
+
+def _stream_of(device):
+    """Current stream of a device that has to be the current one (kernels are launched there)."""
+    torch = _torch()
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ChamError(f"tensors on {device}, current device cuda:{torch.cuda.current_device()}")
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _addr(t, device, what: str, dtype=None, shape=None):
+    """Address of an optional tensor that has to lie on `device`, dense, with this type and shape."""
+    if t is None:
+        return None
+    if t.device != device or (dtype is not None and t.dtype != dtype) or (shape is not None and tuple(t.shape) != tuple(shape)) \
+            or not t.is_contiguous():
+        raise ChamError(f"{what}: need a dense {dtype} tensor of shape {tuple(shape) if shape is not None else 'any'} on {device}, "
+                        f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _scratch(workspace, nbytes: int, device):
+    torch = _torch()
+    if workspace is None or workspace.numel() < nbytes:
+        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    return workspace
+
+
+def _heads(logits, what: str):
+    """(R, G, V, ld_r, ld_g) of logits [R, V] or [R, G, V] whose choices are consecutive."""
+    if logits.dim() not in (2, 3) or (logits.shape[-1] > 1 and logits.stride(-1) != 1):
+        raise ChamError(f"{what}: need [R, V] or [R, G, V] with consecutive choices, got {tuple(logits.shape)} strides {logits.stride()}")
+    R, V = logits.shape[0], logits.shape[-1]
+    return (R, 1, V, logits.stride(0), 0) if logits.dim() == 2 else (R, logits.shape[1], V, logits.stride(0), logits.stride(1))
+
+
+def cham_policy_workspace_bytes(R: int, G: int, V: int, type: int, want_grad: bool) -> int:
+    return _check(load().cham_policy_workspace_bytes(R, G, V, type, 1 if want_grad else 0))
+
+
+def cham_policy_logp(logits, actions, first_action: int = 0, weights=None, out: Optional[dict] = None, workspace=None):
+    """Log-probability of the actions and entropy per decision.  logits [R, V] or [R, G, V] (f32, bf16, f16; choices
+    consecutive), actions [R] or [R, G] (int8, int32, int64); returns a dict of float tensors logp [R], entropy [R]."""
+    torch = _torch()
+    dev = logits.device
+    stream = _stream_of(dev)
+    R, G, V, ld_r, ld_g = _heads(logits, "logits")
+    code = _type_of(logits, _FLOAT_TYPES, "logits")
+    acts = _addr(actions, dev, "actions", None, logits.shape[:-1])
+    out = dict(out) if out is not None else dict(logp=torch.empty(R, dtype=torch.float32, device=dev), entropy=torch.empty(R, dtype=torch.float32, device=dev))
+    workspace = _scratch(workspace, cham_policy_workspace_bytes(R, G, V, code, False), dev)
+    _check(load().cham_policy_logp(logits.data_ptr(), code, R, G, V, ld_r, ld_g, acts, _type_of(actions, _ACTION_TYPES, "actions"), first_action,
+                                   _addr(weights, dev, "weights", torch.float32, (R,)), _addr(out["logp"], dev, "logp", torch.float32, (R,)),
+                                   _addr(out.get("entropy"), dev, "entropy", torch.float32, (R,)),
+                                   _addr(workspace, dev, "workspace", torch.uint8), workspace.numel(), stream))
+    out["workspace"] = workspace
+    return out
+
+
+def cham_policy_loss(logits, actions, old_logp, advantages, first_action: int = 0, ref_logp=None, weights=None, values=None, old_values=None,
+                     returns=None, clip_low: float = 0.2, clip_high: float = 0.2, value_coef: float = 0.0, entropy_coef: float = 0.0,
+                     kl_coef: float = 0.0, value_clip: float = 0.2, want_grad: bool = True, out: Optional[dict] = None, workspace=None):
+    """Clipped policy loss and its gradients; returns a dict of device tensors: terms [6] (names: TERMS), logp and entropy [R],
+    grad_logits (like logits) and grad_values [R] (None without want_grad, or without values).  ``out`` holds the caller's
+    tensors under these names; out["grad_logits"] may be the logits themselves."""
+    torch = _torch()
+    dev = logits.device
+    stream = _stream_of(dev)
+    R, G, V, ld_r, ld_g = _heads(logits, "logits")
+    code = _type_of(logits, _FLOAT_TYPES, "logits")
+    f32 = torch.float32
+    acts = _addr(actions, dev, "actions", None, logits.shape[:-1])
+    if out is None:
+        rows = torch.empty((2, R), dtype=f32, device=dev)
+        out = dict(terms=torch.empty(len(TERMS), dtype=f32, device=dev), logp=rows[0], entropy=rows[1],
+                   grad_logits=torch.empty(logits.shape, dtype=logits.dtype, device=dev) if want_grad else None,
+                   grad_values=torch.empty(R, dtype=f32, device=dev) if want_grad and values is not None else None)
+    else:
+        out = dict(out)
+    grad = out.get("grad_logits") if want_grad else None
+    gld_r = gld_g = 0
+    if grad is not None:
+        if grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != dev:
+            raise ChamError(f"grad_logits: need {logits.dtype} {tuple(logits.shape)} on {dev}, got {grad.dtype} {tuple(grad.shape)} on {grad.device}")
+        _, _, _, gld_r, gld_g = _heads(grad, "grad_logits")
+    coef = _PolicyCoef(clip_low, clip_high, value_coef, entropy_coef, kl_coef, value_clip)
+    workspace = _scratch(workspace, cham_policy_workspace_bytes(R, G, V, code, grad is not None), dev)
+    row = (R,)
+    _check(load().cham_policy_loss(
+        logits.data_ptr(), code, R, G, V, ld_r, ld_g, acts, _type_of(actions, _ACTION_TYPES, "actions"), first_action,
+        _addr(weights, dev, "weights", f32, row), _addr(old_logp, dev, "old_logp", f32, row), _addr(advantages, dev, "advantages", f32, row),
+        _addr(ref_logp, dev, "ref_logp", f32, row), _addr(values, dev, "values", f32, row), _addr(old_values, dev, "old_values", f32, row),
+        _addr(returns, dev, "returns", f32, row), C.byref(coef), _addr(out["terms"], dev, "terms", f32, (len(TERMS),)),
+        _addr(out.get("logp"), dev, "logp", f32, row), _addr(out.get("entropy"), dev, "entropy", f32, row),
+        None if grad is None else grad.data_ptr(), gld_r, gld_g,
+        _addr(out.get("grad_values"), dev, "grad_values", f32, row) if want_grad else None,
+        _addr(workspace, dev, "workspace", torch.uint8), workspace.numel(), stream))
+    out["workspace"] = workspace
+    return out
+
+
+def _matrix(t, device, what: str, dtype, shape):
+    """(address, stride of trajectories, stride of steps) of an optional [B, S] tensor of any strides."""
+    if t is None:
+        return None, 0, 0
+    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ChamError(f"{what}: need {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def cham_gae_workspace_bytes(B: int, S: int) -> int:
+    return _check(load().cham_gae_workspace_bytes(B, S))
+
+
+def cham_gae(rewards, values, gamma: float, lam: float, dones=None, bootstrap=None, lengths=None, out: Optional[dict] = None, workspace=None):
+    """Advantages and returns [B, S] of trajectories; rewards and values [B, S] of one type (f32, bf16, f16), dones uint8
+    or bool [B, S], bootstrap float [B], lengths int32 [B].  Any strides: steps that are stored first ([S, B]) are passed as ``t()``.
+    ``out`` holds advantages and returns (float, of one layout; returns may be None); without it they are made like
+    rewards, zero behind a length."""
+    torch = _torch()
+    dev = rewards.device
+    stream = _stream_of(dev)
+    if rewards.dim() != 2:
+        raise ChamError(f"rewards: need [B, S], got {tuple(rewards.shape)}")
+    B, S = rewards.shape
+    shape = (B, S)
+    code = _type_of(rewards, _FLOAT_TYPES, "rewards")
+    if dones is not None and dones.dtype == torch.bool:
+        dones = dones.view(torch.uint8)
+    if out is None:
+        make = torch.empty if lengths is None else torch.zeros
+        pair = make((2, S, B), dtype=torch.float32, device=dev).transpose(1, 2) if rewards.stride(0) < rewards.stride(1) else make((2, B, S), dtype=torch.float32, device=dev)
+        out = dict(advantages=pair[0], returns=pair[1])
+    else:
+        out = dict(out)
+    r, r_b, r_s = _matrix(rewards, dev, "rewards", rewards.dtype, shape)
+    v, v_b, v_s = _matrix(values, dev, "values", rewards.dtype, shape)
+    d, d_b, d_s = _matrix(dones, dev, "dones", torch.uint8, shape)
+    adv, o_b, o_s = _matrix(out["advantages"], dev, "advantages", torch.float32, shape)
+    ret, q_b, q_s = _matrix(out.get("returns"), dev, "returns", torch.float32, shape)
+    if ret is not None and (q_b, q_s) != (o_b, o_s):
+        raise ChamError("returns: need the strides of advantages")
+    workspace = _scratch(workspace, cham_gae_workspace_bytes(B, S), dev)
+    _check(load().cham_gae(code, B, S, r, r_b, r_s, v, v_b, v_s, d, d_b, d_s, _addr(bootstrap, dev, "bootstrap", torch.float32, (B,)),
+                           _addr(lengths, dev, "lengths", torch.int32, (B,)), gamma, lam, adv, ret, o_b, o_s,
+                           _addr(workspace, dev, "workspace", torch.uint8), workspace.numel(), stream))
+    out["workspace"] = workspace
+    return out
+
+
+class GradList:
+    """Addresses, sizes and types of a list of dense tensors on one device, for programs that clip the same tensors in every
+    step.  It keeps the tensors alive; a tensor whose storage is replaced needs a new list."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        n = len(self.tensors)
+        self.n = n
+        self.device = self.tensors[0].device if n else None
+        codes = []
+        for i, t in enumerate(self.tensors):
+            if t.device != self.device or not t.is_contiguous():
+                raise ChamError(f"tensor {i}: need dense tensors on one device, got strides {t.stride()} on {t.device}")
+            codes.append(_type_of(t, _FLOAT_TYPES, f"tensor {i}"))
+        self.ptrs = (C.c_void_p * max(n, 1))(*[t.data_ptr() for t in self.tensors])
+        self.numels = (C.c_int64 * max(n, 1))(*[t.numel() for t in self.tensors])
+        self.types = (C.c_int32 * max(n, 1))(*codes)
+        self.workspace_bytes = _check(load().cham_grad_workspace_bytes(self.numels, self.types, n))
+
+
+def _grad_call(grads, norm, workspace):
+    torch = _torch()
+    grads = grads if isinstance(grads, GradList) else GradList(grads)
+    dev = grads.device if grads.n else torch.device("cuda", torch.cuda.current_device())
+    stream = _stream_of(dev)
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float64, device=dev)
+    workspace = _scratch(workspace, grads.workspace_bytes, dev)
+    return grads, norm, _addr(norm, dev, "norm", torch.float64, (1,)), workspace, _addr(workspace, dev, "workspace", torch.uint8), stream
+
+
+def cham_grad_workspace_bytes(grads) -> int:
+    return (grads if isinstance(grads, GradList) else GradList(grads)).workspace_bytes
+
+
+def cham_grad_norm(grads, norm=None, workspace=None):
+    """Norm of all tensors of ``grads`` (a GradList or a list of tensors) together; returns a dict: norm (double [1])."""
+    grads, norm, norm_at, workspace, at, stream = _grad_call(grads, norm, workspace)
+    _check(load().cham_grad_norm(grads.ptrs, grads.numels, grads.types, grads.n, norm_at, at, workspace.numel(), stream))
+    return dict(norm=norm, workspace=workspace)
+
+
+def cham_clip_grads(grads, max_norm: float, out=None, norm=None, norm_given: bool = False, workspace=None):
+    """Scales ``grads`` (a GradList or a list of tensors) to a norm of at most max_norm, in place or into the tensors of
+    ``out``; norm_given: ``norm`` is read instead of computed.  Returns a dict: norm (double [1], before clipping)."""
+    if norm_given and norm is None:
+        raise ChamError("norm_given without a norm")
+    grads, norm, norm_at, workspace, at, stream = _grad_call(grads, norm, workspace)
+    outs = None
+    if out is not None:
+        out = out if isinstance(out, GradList) else GradList(out)
+        if out.n != grads.n or (out.n and out.device != grads.device) or bytes(out.numels) != bytes(grads.numels) or bytes(out.types) != bytes(grads.types):
+            raise ChamError("out: need tensors of the same sizes, types and device as the gradients")
+        outs = out.ptrs
+    _check(load().cham_clip_grads(grads.ptrs, outs, grads.numels, grads.types, grads.n, max_norm, norm_at, at, workspace.numel(),
+                                  F_NORM_GIVEN if norm_given else 0, stream))
+    return dict(norm=norm, workspace=workspace)
+
 
 
 class DeviceWorkload:

@@ -8,7 +8,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcham.so")
-SOURCES = ["cham_api.hip", "lloyd_resident.hip", "lloyd_mfma.hip", "lloyd_stream.hip", "select_snap_synth.hip"]
+SOURCES = ["cham_api.hip", "lloyd_resident.hip", "lloyd_mfma.hip", "lloyd_stream.hip", "select_snap_synth.hip",
+           "explore_api.hip", "policy.hip", "advantages.hip", "grad_clip.hip"]
+HOST_SOURCES = ["cham_api.hip", "explore_api.hip"]       # argument checks, planning, staging
 
 # -ffp-contract=off: the exact re-evaluation must not fuse multiply and add; fused operations
 # in the screening code are written explicitly.  Packed fp32 instructions are switched off.
@@ -40,7 +42,7 @@ def build_lib(verbose: bool = False, extra=()) -> str:
 
 
 def build_host_sanitized(outdir: str) -> str:
-    """A copy of the library whose host code in cham_api.hip (argument checks, planning, staging)
+    """A copy of the library whose host code in HOST_SOURCES (argument checks, planning, staging)
     is built with AddressSanitizer and UndefinedBehaviorSanitizer; device code and the other
     objects are the ordinary ones.  For the CPU-only driver csrc/host_check.c; never loaded by the
     product."""
@@ -48,8 +50,8 @@ def build_host_sanitized(outdir: str) -> str:
     objs = []
     for src in SOURCES:
         obj = os.path.join(CSRC, src.replace(".hip", ".o"))
-        if src == "cham_api.hip":
-            obj = os.path.join(outdir, "cham_api_san.o")
+        if src in HOST_SOURCES:
+            obj = os.path.join(outdir, src.replace(".hip", "_san.o"))
             san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
                    "-Xarch_host", "-fno-sanitize-recover=all", "-g"]
             subprocess.run([hipcc, *FLAGS, *san, "-c", os.path.join(CSRC, src), "-o", obj], check=True)

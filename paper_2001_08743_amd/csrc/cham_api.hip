@@ -6,18 +6,21 @@
 #include <string.h>
 
 #include "cham_internal.h"
+#include "explore.h"
 
 namespace cham {
 
 namespace {
-
 thread_local int32_t g_last_hip = 0;
+}  // namespace
 
 int32_t hip_fail(hipError_t e)
 {
     g_last_hip = (int32_t)e;
     return CHAM_E_HIP;
 }
+
+namespace {
 
 constexpr int64_t kAlign = 256;
 inline int64_t up(int64_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
@@ -347,6 +350,8 @@ const char *cham_strerror(int32_t code)
     case CHAM_E_BAD_FLAG: return "unknown flag bits or init mode";
     case CHAM_E_NOMEM: return "out of host memory for the call's small tables";
     case CHAM_E_TOO_LARGE: return "input needs more scratch memory than the library's static buffer holds (use the entry point that takes a workspace)";
+    case CHAM_E_BAD_TYPE: return "a type that the entry point does not take";
+    case CHAM_E_BAD_COEF: return "a coefficient that is not finite or outside its range";
     default: return "unknown error code";
     }
 }
