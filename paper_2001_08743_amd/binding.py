@@ -43,6 +43,9 @@ class ChamError(RuntimeError):
     pass
 
 
+_FLOAT_TYPES, _ACTION_TYPES = {}, {}                    # torch's types and the library's codes, once torch is there
+
+
 class _PolicyCoef(C.Structure):
     _fields_ = [(name, C.c_double) for name in ("clip_low", "clip_high", "value", "entropy", "kl", "value_clip")]
 
@@ -173,11 +176,19 @@ def _check(rc: int):
     return rc
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    if not torch.cuda.is_available():
-        raise ChamError("no GPU visible: libcham has no CPU path")
-    return torch
+    global _torch_module
+    if _torch_module is None:                           # a GPU that is there stays: asked once, 2 us a call otherwise
+        import torch
+        if not torch.cuda.is_available():
+            raise ChamError("no GPU visible: libcham has no CPU path")
+        _FLOAT_TYPES.update({torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16})
+        _ACTION_TYPES.update({torch.int8: TYPE_I8, torch.int32: TYPE_I32, torch.int64: TYPE_I64})
+        _torch_module = torch
+    return _torch_module
 
 
 def _hp(a: Optional[np.ndarray]):
@@ -561,14 +572,10 @@ def cham_update_configs(theta, actions, cards, salt: int = 0, seen_table=None, u
     return theta
 
 
-_FLOAT_TYPES = {"torch.float32": TYPE_F32, "torch.bfloat16": TYPE_BF16, "torch.float16": TYPE_F16}
-_ACTION_TYPES = {"torch.int8": TYPE_I8, "torch.int32": TYPE_I32, "torch.int64": TYPE_I64}
-
-
 def _type_of(t, types, what: str) -> int:
-    code = types.get(str(t.dtype))
+    code = types.get(t.dtype)
     if code is None:
-        raise ChamError(f"{what}: {t.dtype} is not one of {', '.join(types)}")
+        raise ChamError(f"{what}: {t.dtype} is not one of {', '.join(map(str, types))}")
     return code
 
 
@@ -577,25 +584,26 @@ def _stream_of(device):
     torch = _torch()
     if device.type != "cuda" or device.index != torch.cuda.current_device():
         raise ChamError(f"tensors on {device}, current device cuda:{torch.cuda.current_device()}")
-    return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
-def _addr(t, device, what: str, dtype=None, shape=None):
+def _addr(t, device, what: str, dtype, shape):
     """Address of an optional tensor that has to lie on `device`, dense, with this type and shape."""
     if t is None:
         return None
-    if t.device != device or (dtype is not None and t.dtype != dtype) or (shape is not None and tuple(t.shape) != tuple(shape)) \
-            or not t.is_contiguous():
-        raise ChamError(f"{what}: need a dense {dtype} tensor of shape {tuple(shape) if shape is not None else 'any'} on {device}, "
-                        f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ChamError(f"{what}: need a dense {dtype} tensor of shape {tuple(shape)} on {device}, "
+                    f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
 
 
-def _scratch(workspace, nbytes: int, device):
-    torch = _torch()
-    if workspace is None or workspace.numel() < nbytes:
-        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-    return workspace
+def _scratch(workspace, device, nbytes, *sizes):
+    """The caller's workspace, or one of nbytes(*sizes) bytes; and its address."""
+    if workspace is None:
+        workspace = _torch().empty(max(nbytes(*sizes), 256), dtype=_torch().uint8, device=device)
+    elif workspace.device != device or not workspace.is_contiguous() or workspace.element_size() != 1:
+        raise ChamError(f"workspace: need dense bytes on {device}, got {workspace.dtype} strides {workspace.stride()} on {workspace.device}")
+    return workspace, workspace.data_ptr()
 
 
 def _heads(logits, what: str):
@@ -618,13 +626,12 @@ def cham_policy_logp(logits, actions, first_action: int = 0, weights=None, out: 
     stream = _stream_of(dev)
     R, G, V, ld_r, ld_g = _heads(logits, "logits")
     code = _type_of(logits, _FLOAT_TYPES, "logits")
-    acts = _addr(actions, dev, "actions", None, logits.shape[:-1])
+    acts = _addr(actions, dev, "actions", actions.dtype, logits.shape[:-1])
     out = dict(out) if out is not None else dict(logp=torch.empty(R, dtype=torch.float32, device=dev), entropy=torch.empty(R, dtype=torch.float32, device=dev))
-    workspace = _scratch(workspace, cham_policy_workspace_bytes(R, G, V, code, False), dev)
+    workspace, at = _scratch(workspace, dev, cham_policy_workspace_bytes, R, G, V, code, False)
     _check(load().cham_policy_logp(logits.data_ptr(), code, R, G, V, ld_r, ld_g, acts, _type_of(actions, _ACTION_TYPES, "actions"), first_action,
                                    _addr(weights, dev, "weights", torch.float32, (R,)), _addr(out["logp"], dev, "logp", torch.float32, (R,)),
-                                   _addr(out.get("entropy"), dev, "entropy", torch.float32, (R,)),
-                                   _addr(workspace, dev, "workspace", torch.uint8), workspace.numel(), stream))
+                                   _addr(out.get("entropy"), dev, "entropy", torch.float32, (R,)), at, workspace.numel(), stream))
     out["workspace"] = workspace
     return out
 
@@ -641,7 +648,7 @@ def cham_policy_loss(logits, actions, old_logp, advantages, first_action: int = 
     R, G, V, ld_r, ld_g = _heads(logits, "logits")
     code = _type_of(logits, _FLOAT_TYPES, "logits")
     f32 = torch.float32
-    acts = _addr(actions, dev, "actions", None, logits.shape[:-1])
+    acts = _addr(actions, dev, "actions", actions.dtype, logits.shape[:-1])
     if out is None:
         rows = torch.empty((2, R), dtype=f32, device=dev)
         out = dict(terms=torch.empty(len(TERMS), dtype=f32, device=dev), logp=rows[0], entropy=rows[1],
@@ -656,7 +663,7 @@ def cham_policy_loss(logits, actions, old_logp, advantages, first_action: int = 
             raise ChamError(f"grad_logits: need {logits.dtype} {tuple(logits.shape)} on {dev}, got {grad.dtype} {tuple(grad.shape)} on {grad.device}")
         _, _, _, gld_r, gld_g = _heads(grad, "grad_logits")
     coef = _PolicyCoef(clip_low, clip_high, value_coef, entropy_coef, kl_coef, value_clip)
-    workspace = _scratch(workspace, cham_policy_workspace_bytes(R, G, V, code, grad is not None), dev)
+    workspace, at = _scratch(workspace, dev, cham_policy_workspace_bytes, R, G, V, code, grad is not None)
     row = (R,)
     _check(load().cham_policy_loss(
         logits.data_ptr(), code, R, G, V, ld_r, ld_g, acts, _type_of(actions, _ACTION_TYPES, "actions"), first_action,
@@ -665,8 +672,7 @@ def cham_policy_loss(logits, actions, old_logp, advantages, first_action: int = 
         _addr(returns, dev, "returns", f32, row), C.byref(coef), _addr(out["terms"], dev, "terms", f32, (len(TERMS),)),
         _addr(out.get("logp"), dev, "logp", f32, row), _addr(out.get("entropy"), dev, "entropy", f32, row),
         None if grad is None else grad.data_ptr(), gld_r, gld_g,
-        _addr(out.get("grad_values"), dev, "grad_values", f32, row) if want_grad else None,
-        _addr(workspace, dev, "workspace", torch.uint8), workspace.numel(), stream))
+        _addr(out.get("grad_values"), dev, "grad_values", f32, row) if want_grad else None, at, workspace.numel(), stream))
     out["workspace"] = workspace
     return out
 
@@ -675,9 +681,9 @@ def _matrix(t, device, what: str, dtype, shape):
     """(address, stride of trajectories, stride of steps) of an optional [B, S] tensor of any strides."""
     if t is None:
         return None, 0, 0
-    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.device != device or t.dtype is not dtype or t.shape != shape:
         raise ChamError(f"{what}: need {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return (t.data_ptr(), *t.stride())
 
 
 def cham_gae_workspace_bytes(B: int, S: int) -> int:
@@ -694,8 +700,7 @@ def cham_gae(rewards, values, gamma: float, lam: float, dones=None, bootstrap=No
     stream = _stream_of(dev)
     if rewards.dim() != 2:
         raise ChamError(f"rewards: need [B, S], got {tuple(rewards.shape)}")
-    B, S = rewards.shape
-    shape = (B, S)
+    B, S = shape = rewards.shape
     code = _type_of(rewards, _FLOAT_TYPES, "rewards")
     if dones is not None and dones.dtype == torch.bool:
         dones = dones.view(torch.uint8)
@@ -712,10 +717,10 @@ def cham_gae(rewards, values, gamma: float, lam: float, dones=None, bootstrap=No
     ret, q_b, q_s = _matrix(out.get("returns"), dev, "returns", torch.float32, shape)
     if ret is not None and (q_b, q_s) != (o_b, o_s):
         raise ChamError("returns: need the strides of advantages")
-    workspace = _scratch(workspace, cham_gae_workspace_bytes(B, S), dev)
+    workspace, at = _scratch(workspace, dev, cham_gae_workspace_bytes, B, S)
     _check(load().cham_gae(code, B, S, r, r_b, r_s, v, v_b, v_s, d, d_b, d_s, _addr(bootstrap, dev, "bootstrap", torch.float32, (B,)),
                            _addr(lengths, dev, "lengths", torch.int32, (B,)), gamma, lam, adv, ret, o_b, o_s,
-                           _addr(workspace, dev, "workspace", torch.uint8), workspace.numel(), stream))
+                           at, workspace.numel(), stream))
     out["workspace"] = workspace
     return out
 
@@ -725,6 +730,7 @@ class GradList:
     step.  It keeps the tensors alive; a tensor whose storage is replaced needs a new list."""
 
     def __init__(self, tensors):
+        _torch()
         self.tensors = list(tensors)
         n = len(self.tensors)
         self.n = n
@@ -747,8 +753,8 @@ def _grad_call(grads, norm, workspace):
     stream = _stream_of(dev)
     if norm is None:
         norm = torch.empty(1, dtype=torch.float64, device=dev)
-    workspace = _scratch(workspace, grads.workspace_bytes, dev)
-    return grads, norm, _addr(norm, dev, "norm", torch.float64, (1,)), workspace, _addr(workspace, dev, "workspace", torch.uint8), stream
+    workspace, at = _scratch(workspace, dev, int, grads.workspace_bytes)
+    return grads, norm, _addr(norm, dev, "norm", torch.float64, (1,)), workspace, at, stream
 
 
 def cham_grad_workspace_bytes(grads) -> int:
@@ -777,7 +783,6 @@ def cham_clip_grads(grads, max_norm: float, out=None, norm=None, norm_given: boo
     _check(load().cham_clip_grads(grads.ptrs, outs, grads.numels, grads.types, grads.n, max_norm, norm_at, at, workspace.numel(),
                                   F_NORM_GIVEN if norm_given else 0, stream))
     return dict(norm=norm, workspace=workspace)
-
 
 
 class DeviceWorkload:

@@ -36,6 +36,7 @@ struct PolicyArgs {
 
 // How a call is run; a function of its sizes and type alone, so that the workspace can be asked for ahead of it.
 struct PolicyPlan {
+    int tile;                      // decisions of a tile where heads have few choices; 0: heads in parts
     int splits;                    // workgroups a head is split over
     int chunk;                     // choices each of them takes
     int64_t o_sums, o_part, o_head, o_dec, bytes;

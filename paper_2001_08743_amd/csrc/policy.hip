@@ -157,6 +157,157 @@ __global__ void __launch_bounds__(kThreads) policy_terms_kernel(const PolicyArgs
     }
 }
 
+// --- few choices a head: a workgroup takes whole decisions, a thread whole heads
+
+constexpr int kTileHeads = 1024;                // at most: kHeadsPerThread of each thread
+constexpr int kHeadsPerThread = kTileHeads / kThreads;
+constexpr int kTileItems = 8448;                // fp32 logits in LDS, 33 KiB: four workgroups share a compute unit
+constexpr int kTileChoices = 32;                // beyond, a tile has fewer heads than threads
+
+struct TileShape {
+    int per_tile;           // decisions of a tile
+    int stride;             // of a head's logits in LDS: odd, so that the threads of a wave read different banks
+    unsigned inv_v, inv_gv; // ceil(2^32 / V), ceil(2^32 / (G V)): quotients of item numbers below 2^16
+    int dense;              // the logits of a tile are one run of items
+    int gdense;             // its gradients are
+};
+
+__device__ __forceinline__ int quotient(int i, unsigned inv, int by) { return by == 1 ? i : (int)__umulhi((unsigned)i, inv); }
+
+// Items of a run of n at p, f(index, value), 16 bytes at a time.
+template <typename T, typename F>
+__device__ __forceinline__ void read_run(const typename T::item *p, int n, F &&f)
+{
+    const int head = (int)items_to_boundary<T>(p, n), n_vec = (n - head) / T::kVec, tail = head + n_vec * T::kVec;
+    if ((int)threadIdx.x < head) f((int)threadIdx.x, T::get(p[threadIdx.x]));
+    if ((int)threadIdx.x < n - tail) f(tail + (int)threadIdx.x, T::get(p[tail + threadIdx.x]));
+    const uint4 *body = reinterpret_cast<const uint4 *>(p + head);
+    for (int i = threadIdx.x; i < n_vec; i += kThreads) {
+        float x[T::kVec];
+        T::unpack(body[i], x);
+#pragma unroll
+        for (int j = 0; j < T::kVec; ++j) f(head + i * T::kVec + j, x[j]);
+    }
+}
+template <typename T, typename F>
+__device__ __forceinline__ void write_run(typename T::item *p, int n, F &&f)
+{
+    const int head = (int)items_to_boundary<T>(p, n), n_vec = (n - head) / T::kVec, tail = head + n_vec * T::kVec;
+    if ((int)threadIdx.x < head) p[threadIdx.x] = T::put(f((int)threadIdx.x));
+    if ((int)threadIdx.x < n - tail) p[tail + threadIdx.x] = T::put(f(tail + (int)threadIdx.x));
+    uint4 *body = reinterpret_cast<uint4 *>(p + head);
+    for (int i = threadIdx.x; i < n_vec; i += kThreads) {
+        float x[T::kVec];
+#pragma unroll
+        for (int j = 0; j < T::kVec; ++j) x[j] = f(head + i * T::kVec + j);
+        body[i] = T::pack(x);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs a, const TileShape k)
+{
+    __shared__ float x[kTileItems];
+    __shared__ float2 one[kTileHeads];          // log-probability and entropy of a head
+    __shared__ float2 dec[kTileHeads];          // of a decision: (D, w c_H)
+    __shared__ uint8_t in[kTileHeads];
+    const int tid = threadIdx.x;
+    const int gv = a.G * a.V;
+    double sum[kPolicySums] = {};
+    for (int64_t r0 = (int64_t)blockIdx.x * k.per_tile; r0 < a.R; r0 += (int64_t)gridDim.x * k.per_tile) {
+        const int nr = a.R - r0 < k.per_tile ? (int)(a.R - r0) : k.per_tile;
+        const int heads = nr * a.G, items = nr * gv;
+        auto at = [&](int i) {                  // where item i of the tile stands in LDS
+            const int h = k.stride == a.V ? 0 : quotient(i, k.inv_v, a.V);
+            return i + h;
+        };
+        auto offset = [&](int i, int64_t ld_r, int64_t ld_g) {
+            const int h = quotient(i, k.inv_v, a.V), r = quotient(i, k.inv_gv, gv);
+            return (r0 + r) * ld_r + (h - r * a.G) * ld_g + (i - h * a.V);
+        };
+        const typename T::item *logits = static_cast<const typename T::item *>(a.logits);
+        if (k.dense)
+            read_run<T>(logits + r0 * gv, items, [&](int i, float v) { x[at(i)] = v; });
+        else
+            for (int i = tid; i < items; i += kThreads) x[at(i)] = T::get(logits[offset(i, a.ld_r, a.ld_g)]);
+        __syncthreads();
+
+        float m[kHeadsPerThread], ls[kHeadsPerThread], ent[kHeadsPerThread];
+        int c[kHeadsPerThread];
+#pragma unroll
+        for (int u = 0; u < kHeadsPerThread; ++u) {
+            const int h = tid + u * kThreads;
+            m[u] = ls[u] = ent[u] = 0.0f;
+            c[u] = -1;
+            if (h >= heads) continue;
+            const float *xh = x + h * k.stride;
+            c[u] = choice_of(a, r0 * a.G + h);
+            float lp = 0.0f;
+            if (c[u] == a.V) {
+                c[u] = 0;
+                ls[u] = ent[u] = lp = __builtin_nanf("");
+            } else if (c[u] >= 0) {
+                Soft v = soft_none();
+                for (int j = 0; j < a.V; ++j) v.m = fmaxf(v.m, xh[j]);
+                for (int j = 0; j < a.V; ++j) soft_add(v, xh[j]);
+                if (v.s != 0.0f) {
+                    m[u] = v.m;
+                    ls[u] = logf(v.s);
+                    ent[u] = ls[u] - v.t / v.s;
+                    lp = xh[c[u]] - v.m - ls[u];
+                } else {
+                    c[u] = -1;                  // every choice is masked
+                }
+            }
+            one[h] = make_float2(lp, ent[u]);
+            in[h] = c[u] >= 0;
+        }
+        __syncthreads();
+        for (int r = tid; r < nr; r += kThreads) {
+            double lp = 0.0, H = 0.0;
+            bool any = false;
+            if (counts(a, r0 + r))
+                for (int g = 0; g < a.G; ++g) {
+                    const float2 o = one[r * a.G + g];
+                    lp += (double)o.x;
+                    H += (double)o.y;
+                    any = any || in[r * a.G + g] != 0;
+                }
+            dec[r] = decide(a, r0 + r, any, lp, H, sum);
+            if (!any)                           // also of weight 0: zeros, whatever the logits are
+                for (int g = 0; g < a.G; ++g) in[r * a.G + g] = 0;
+        }
+        if (!a.grad) {
+            __syncthreads();
+            continue;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kHeadsPerThread; ++u) {
+            const int h = tid + u * kThreads;
+            if (h >= heads) continue;
+            float *xh = x + h * k.stride;
+            if (!in[h]) {
+                for (int j = 0; j < a.V; ++j) xh[j] = 0.0f;
+                continue;
+            }
+            const float2 d = dec[a.G == 1 ? h : h / a.G];
+            for (int j = 0; j < a.V; ++j) {
+                const float z = xh[j] - m[u] - ls[u], p = exp_fast(z);
+                xh[j] = (j == c[u] ? d.x : 0.0f) - p * (d.x - d.y * (fmaxf(z, kFar) + ent[u]));
+            }
+        }
+        __syncthreads();
+        typename T::item *grad = static_cast<typename T::item *>(a.grad);
+        if (k.gdense)
+            write_run<T>(grad + r0 * gv, items, [&](int i) { return x[at(i)]; });
+        else
+            for (int i = tid; i < items; i += kThreads) grad[offset(i, a.gld_r, a.gld_g)] = T::put(x[at(i)]);
+        __syncthreads();
+    }
+    if (a.old_logp) store_sums<kThreads / 64>(a, sum);
+}
+
 // --- any number of heads and choices, in three steps: sums of parts of heads, decisions, gradient
 
 // Visits the items [lo, hi) of a row, 16 bytes at a time from the first boundary on; f(index, value).
@@ -276,6 +427,7 @@ __global__ void __launch_bounds__(kThreads) policy_grad_kernel(const PolicyArgs 
 }
 
 constexpr int kJoinBlocks = 1024;
+constexpr int kTileBlocks = 1024;               // what is on the chip at a time
 constexpr unsigned kMostBlocks = 1u << 20;
 
 unsigned blocks_for(int64_t n) { return (unsigned)(n < (int64_t)kMostBlocks ? n : (int64_t)kMostBlocks); }
@@ -284,6 +436,21 @@ int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 template <typename T>
 hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
 {
+    if (p.tile) {
+        const int gv = a.G * a.V;
+        TileShape k;
+        k.per_tile = p.tile;
+        k.stride = a.V | 1;
+        k.inv_v = (unsigned)((((uint64_t)1 << 32) + a.V - 1) / a.V);
+        k.inv_gv = (unsigned)((((uint64_t)1 << 32) + gv - 1) / gv);
+        k.dense = (a.G == 1 || a.ld_g == a.V) && (a.R == 1 || a.ld_r == gv);
+        k.gdense = (a.G == 1 || a.gld_g == a.V) && (a.R == 1 || a.gld_r == gv);
+        const int64_t tiles = (a.R + p.tile - 1) / p.tile;
+        const unsigned blocks = (unsigned)(tiles < kTileBlocks ? tiles : kTileBlocks);
+        if (a.R > 0) hipLaunchKernelGGL(policy_tile_kernel<T>, dim3(blocks), dim3(kThreads), 0, s, a, k);
+        if (a.old_logp) hipLaunchKernelGGL(policy_terms_kernel, dim3(1), dim3(kThreads), 0, s, a, (int)blocks);
+        return hipGetLastError();
+    }
     const int64_t units = a.R * a.G * p.splits;
     const unsigned join = (unsigned)((a.R + 3) / 4 < kJoinBlocks ? (a.R + 3) / 4 : kJoinBlocks);
     if (a.R > 0) {
@@ -299,7 +466,13 @@ hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
 
 PolicyPlan plan_policy(int64_t R, int G, int V, int type, bool grad)
 {
-    PolicyPlan p;
+    PolicyPlan p{};
+    if (V <= kTileChoices && G <= kTileHeads && (int64_t)G * (V | 1) <= kTileItems) {
+        const int by_heads = kTileHeads / G, by_items = kTileItems / (G * (V | 1));
+        p.tile = by_heads < by_items ? by_heads : by_items;
+        p.bytes = (int64_t)kTileBlocks * kPolicySums * 8;
+        return p;
+    }
     // parts of a head: of at least 4096 choices, until there are 1024 workgroups
     const int64_t heads = R * G;
     int64_t most = ((int64_t)V + 4095) / 4096;

@@ -171,6 +171,14 @@ def test_left_out_heads_and_decisions(R, G, V):
     _check_policy(got, lp, H, G, V)
 
 
+@pytest.mark.parametrize("R,G,V", [(50, 5, 3), (50, 1, 700), (5, 1, 40001), (5, 2, 9000)])
+def test_weights_of_either_sign(R, G, V):
+    x, a = _policy_inputs(R, G, V, torch.float32, 23)
+    w = torch.randn(R, generator=_gen(24))
+    got, want = _run_loss(x, a, _loss_inputs(x, a, 0, 25), weights=w)
+    _check_loss(got, want, G, V)
+
+
 @pytest.mark.parametrize("R,G,V", [(9, 5, 3), (9, 1, 700), (5, 1, 40001), (5, 2, 9000)])
 def test_what_is_no_number_stays_in_its_decision(R, G, V):
     x, a = _policy_inputs(R, G, V, torch.float32, 31)
