@@ -36,7 +36,8 @@ struct PolicyArgs {
 
 // How a call is run; a function of its sizes and type alone, so that the workspace can be asked for ahead of it.
 struct PolicyPlan {
-    int tile;                      // decisions of a tile where heads have few choices; 0: heads in parts
+    int tile;                      // few choices a head: decisions of a tile; 0 elsewhere
+    int row, threads;              // one head: 16-byte pieces of a row that each of so many threads holds; 0 elsewhere
     int splits;                    // workgroups a head is split over
     int chunk;                     // choices each of them takes
     int64_t o_sums, o_part, o_head, o_dec, bytes;

@@ -7,9 +7,13 @@
 
 namespace cham {
 
+typedef float float2v __attribute__((ext_vector_type(2)));
+
 struct F32 {
     using item = float;
+    typedef unsigned words __attribute__((ext_vector_type(4), aligned(4)));         // 16 bytes that begin at any item
     static constexpr int kVec = 4;              // items in 16 bytes
+    static constexpr uint32_t kMasked = 0xff800000u;         // -inf
     static __device__ __forceinline__ float get(item x) { return x; }
     static __device__ __forceinline__ item put(float x) { return x; }
     static __device__ __forceinline__ void unpack(const uint4 &v, float (&x)[4])
@@ -27,7 +31,9 @@ struct F32 {
 
 struct BF16 {
     using item = __bf16;
+    typedef unsigned words __attribute__((ext_vector_type(4), aligned(2)));
     static constexpr int kVec = 8;
+    static constexpr uint32_t kMasked = 0xff80u;
     static __device__ __forceinline__ float get(item x) { return (float)x; }
     static __device__ __forceinline__ item put(float x) { return (item)x; }        // to the nearest, ties to even
     static __device__ __forceinline__ void unpack(const uint4 &v, float (&x)[8])
@@ -45,8 +51,8 @@ struct BF16 {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const b2 p = {(__bf16)x[2 * i], (__bf16)x[2 * i + 1]};
-            w[i] = __builtin_bit_cast(uint32_t, p);
+            const float2v p = {x[2 * i], x[2 * i + 1]};                            // both in one instruction
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, b2));
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -54,7 +60,9 @@ struct BF16 {
 
 struct F16 {
     using item = _Float16;
+    typedef unsigned words __attribute__((ext_vector_type(4), aligned(2)));
     static constexpr int kVec = 8;
+    static constexpr uint32_t kMasked = 0xfc00u;
     // x as fp32: the compiler folds a product and its rounding to f16 into one operation where it can, which depends on the
     // code around it, and a result would depend on the alignment of its row
     static __device__ __forceinline__ float held(float x)
@@ -81,8 +89,8 @@ struct F16 {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const h2 p = {put(x[2 * i]), put(x[2 * i + 1])};
-            w[i] = __builtin_bit_cast(uint32_t, p);
+            const float2v p = {held(x[2 * i]), held(x[2 * i + 1])};
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, h2));
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }

@@ -5,7 +5,9 @@
 // H = log s - t / s.  Per decision, lp = sum over heads of log p_action, and with ratio rho = e^(lp - old)
 //   L = w (-min(rho A, clip(rho) A) + c_v value - c_H H + c_kl (e^d - d - 1)),   d = ref - lp
 //   dL/dlp = D = w (-rho A [unclipped side] + c_kl (1 - e^d)),   dL/dx_v = D ([v = a] - p_v) + w c_H p_v (log p_v + H).
-// Exponentials and their sums are fp32 (logits have at most 24 bits), everything per decision double.
+// Exponentials are fp32 (logits have at most 24 bits), and the sums of a head; differences, products and sums per decision and
+// beyond are double.  Double exponentials would change nothing that a log-probability from fp32 sums does not blur, and their
+// constants, held in registers across the rows of a workgroup, took 60 registers of the kernels that hold a row.
 #include "cham_device.h"
 #include "explore.h"
 #include "explore_items.h"
@@ -16,11 +18,25 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr float kLowest = -3.402823466e38f;     // maximum of nothing: finite, so that -inf - kLowest is not a NaN
-constexpr float kFar = -200.0f;                 // e^x is 0 in fp32 below; keeps 0 * (-inf) out of the sums
+constexpr float kFar = -300.0f;                 // 2^x is 0 in fp32 below; keeps 0 * (-inf) out of the sums
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
-__device__ __forceinline__ float exp_fast(float z) { return __builtin_amdgcn_exp2f(z * 1.44269504f); }
+__device__ __forceinline__ float exp2_fast(float z) { return __builtin_amdgcn_exp2f(z); }
 
-// Running maximum and sums of a head.
+// Exponents are taken to the base 2: z = x k - m k, k = log2 e, one fused operation and no rounding but its own; the
+// rounding of m k is common to a head's exponentials and drops out.  Where m k would overflow k is 1: logits that far out are
+// alike or 2^103 apart.
+struct Scale {
+    float k, mk;
+};
+__device__ __forceinline__ Scale scale_of(float m)
+{
+    const float k = fabsf(m) > 1e38f ? 1.0f : kLog2e;
+    return {k, m * k};
+}
+__device__ __forceinline__ float exponent(float x, const Scale &k) { return __builtin_fmaf(x, k.k, -k.mk); }
+
+// Running maximum and sums of a head: of 2^z and of z 2^z.
 struct Soft {
     float m, s, t;
 };
@@ -29,17 +45,32 @@ __device__ __forceinline__ Soft soft_none() { return {kLowest, 0.0f, 0.0f}; }
 __device__ __forceinline__ void soft_raise(Soft &a, float m)
 {
     if (m > a.m) {
-        const float d = a.m - m, f = exp_fast(d);
+        const float d = (a.m - m) * kLog2e, f = exp2_fast(d);
         a.t = f > 0.0f ? f * (a.t + a.s * d) : 0.0f;
         a.s *= f;
         a.m = m;
     }
 }
-__device__ __forceinline__ void soft_add(Soft &a, float x)
+__device__ __forceinline__ void soft_add(Soft &a, float x, const Scale &k)
 {
-    const float z = x - a.m, e = exp_fast(z);
+    const float z = exponent(x, k), e = exp2_fast(z);
     a.s += e;
-    a.t += e * fmaxf(z, kFar);
+    a.t = __builtin_fmaf(e, fmaxf(z, kFar), a.t);
+}
+// N items more; k = scale_of(a.m).  m is raised when an item is more than 8 above it and not before: e^8 times V stays far inside
+// fp32, and lanes that each find a new maximum now and then would have the wave rescale all the time.
+template <int N>
+__device__ __forceinline__ void soft_add_all(Soft &a, Scale &k, const float (&x)[N])
+{
+    float m = x[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
+    if (m > a.m + 8.0f) {
+        soft_raise(a, m);
+        k = scale_of(a.m);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) soft_add(a, x[j], k);
 }
 __device__ __forceinline__ Soft soft_join(Soft a, Soft b)
 {
@@ -48,11 +79,62 @@ __device__ __forceinline__ Soft soft_join(Soft a, Soft b)
     soft_raise(b, m);
     return {m, a.s + b.s, a.t + b.t};
 }
+
+// log s and entropy of a head's sums (s > 0).
+__device__ __forceinline__ float2 log_and_entropy(const Soft &v)
+{
+    const float ls = logf(v.s);
+    return make_float2(ls, ls - v.t * kLn2 / v.s);
+}
+
+// Gradient by a head's logits: 2^z (c0 + c1 z), and D more at the action.
+struct Slope {
+    Scale k;
+    float c0, c1;
+};
+__device__ __forceinline__ Slope slope_of(float m, float s, float ls, float entropy, float2 d)
+{
+    const float inv = 1.0f / s;
+    return {scale_of(m), (d.y * (entropy - ls) - d.x) * inv, d.y * kLn2 * inv};
+}
+template <bool ENT>
+__device__ __forceinline__ float slope_at(const Slope &f, float x)
+{
+    const float z = exponent(x, f.k), e = exp2_fast(z);
+    return ENT ? e * __builtin_fmaf(fmaxf(z, kFar), f.c1, f.c0) : e * f.c0;
+}
+
+// Maximum and sum over a wave, in every lane: within rows of sixteen lanes, then across rows, by lane shifts.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float shifted(float x, float none)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_max(float x)
+{
+    x = fmaxf(x, shifted<0x111, 0xf>(x, x));       // row_shr 1, 2, 4, 8
+    x = fmaxf(x, shifted<0x112, 0xf>(x, x));
+    x = fmaxf(x, shifted<0x114, 0xf>(x, x));
+    x = fmaxf(x, shifted<0x118, 0xf>(x, x));
+    x = fmaxf(x, shifted<0x142, 0xa>(x, x));       // row_bcast 15, 31
+    x = fmaxf(x, shifted<0x143, 0xc>(x, x));
+    return readlane_f(x, 63);
+}
+__device__ __forceinline__ float wave_sum_f(float x)
+{
+    x += shifted<0x111, 0xf>(x, 0.0f);
+    x += shifted<0x112, 0xf>(x, 0.0f);
+    x += shifted<0x114, 0xf>(x, 0.0f);
+    x += shifted<0x118, 0xf>(x, 0.0f);
+    x += shifted<0x142, 0xa>(x, 0.0f);
+    x += shifted<0x143, 0xc>(x, 0.0f);
+    return readlane_f(x, 63);
+}
+// One maximum for all lanes first, so that each rescales its sums once.
 __device__ __forceinline__ Soft soft_wave(Soft a)
 {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) a = soft_join(a, {__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.t, o)});
-    return a;
+    soft_raise(a, wave_max(a.m));
+    return {a.m, wave_sum_f(a.s), wave_sum_f(a.t)};
 }
 
 // Choice of an action: -1 = its head is left out, V = outside the choices.
@@ -68,30 +150,71 @@ __device__ __forceinline__ int choice_of(const PolicyArgs &a, int64_t i)
 
 __device__ __forceinline__ bool counts(const PolicyArgs &a, int64_t r) { return !a.weights || a.weights[r] != 0.0f; }
 
-// One decision: writes its outputs, adds its terms, returns (D, w c_H).
-__device__ __forceinline__ float2 decide(const PolicyArgs &a, int64_t r, bool in, double lp, double H, double (&sum)[kPolicySums])
+// e^d - 1 - d, e = e^d - 1.  Near 0 by its series, which loses nothing to the difference (|d| <= 1/4: the first term left out is
+// below 2^-24 of the sum).
+__device__ __forceinline__ float divergence(float d, float e)
 {
-    if (a.logp) a.logp[r] = in ? (float)lp : 0.0f;
-    if (a.entropy) a.entropy[r] = in ? (float)H : 0.0f;
+    if (fabsf(d) <= 0.25f) {
+        float p = 1.0f / 40320.0f;
+        p = __builtin_fmaf(p, d, 1.0f / 5040.0f);
+        p = __builtin_fmaf(p, d, 1.0f / 720.0f);
+        p = __builtin_fmaf(p, d, 1.0f / 120.0f);
+        p = __builtin_fmaf(p, d, 1.0f / 24.0f);
+        p = __builtin_fmaf(p, d, 1.0f / 6.0f);
+        p = __builtin_fmaf(p, d, 0.5f);
+        return p * d * d;
+    }
+    return e < __builtin_inff() ? e - d : e;           // an action that the policy has lost: infinite, not inf - inf
+}
+
+// What a decision is compared with.
+struct Given {
+    float w, adv, old, ref, value, old_value, ret;
+};
+template <typename LOAD>
+__device__ __forceinline__ Given given_of(const PolicyArgs &a, int64_t r, LOAD &&load)
+{
+    Given g{};
+    if (!a.old_logp) return g;
+    g.old = load(a.old_logp, r);
+    g.adv = load(a.adv, r);
+    if (a.weights) g.w = load(a.weights, r);
+    if (a.ref) g.ref = load(a.ref, r);
+    if (a.values) {
+        g.value = load(a.values, r);
+        g.ret = load(a.returns, r);
+        if (a.old_values) g.old_value = load(a.old_values, r);
+    }
+    return g;
+}
+__device__ __forceinline__ float load_plain(const float *p, int64_t i) { return p[i]; }
+// By way of the scalar cache: for a decision that all lanes share.  Nothing that this reads is written by the kernel.
+__device__ __forceinline__ float load_shared(const float *p, int64_t i) { return reinterpret_cast<const __attribute__((address_space(4))) float *>((uintptr_t)p)[i]; }
+
+// One decision: writes its outputs, adds its terms, returns (D, w c_H).
+__device__ __forceinline__ float2 decide(const PolicyArgs &a, int64_t r, const Given &in, bool on, double lp, double H, double *sum)
+{
+    if (a.logp) a.logp[r] = on ? (float)lp : 0.0f;
+    if (a.entropy) a.entropy[r] = on ? (float)H : 0.0f;
     if (!a.old_logp) return make_float2(0.0f, 0.0f);
-    if (!in) {
+    if (!on) {
         if (a.grad_values) a.grad_values[r] = 0.0f;
         return make_float2(0.0f, 0.0f);
     }
-    const double w = a.weights ? (double)a.weights[r] : a.w_all;
-    const double A = (double)a.adv[r];
-    const double rho = exp(lp - (double)a.old_logp[r]);
+    const double w = a.weights ? (double)in.w : a.w_all;
+    const double A = (double)in.adv;
+    const double rho = (double)expf((float)(lp - (double)in.old));
     const double held_rho = rho < a.lo ? a.lo : rho > a.hi ? a.hi : rho;
     const double free = rho * A, held = held_rho * A;
     const bool clipped = free > held;
     sum[0] -= w * (clipped ? held : free);
     double D = clipped ? 0.0 : -free;
     if (a.values) {
-        const double v = (double)a.values[r], ret = (double)a.returns[r];
+        const double v = (double)in.value, ret = (double)in.ret;
         const double near = (v - ret) * (v - ret);
         double kept = near;
         if (a.old_values) {
-            const double o = (double)a.old_values[r], d = v - o;
+            const double o = (double)in.old_value, d = v - o;
             const double k = o + (d < -a.value_clip ? -a.value_clip : d > a.value_clip ? a.value_clip : d) - ret;
             kept = k * k;
         }
@@ -102,15 +225,44 @@ __device__ __forceinline__ float2 decide(const PolicyArgs &a, int64_t r, bool in
     }
     sum[2] += w * H;
     if (a.ref) {
-        const double d = (double)a.ref[r] - lp, e = expm1(d);
-        sum[3] += w * (e < __builtin_inf() ? e - d : e);      // an action that the policy has lost: infinite, not inf - inf
-        if (a.c_kl != 0.0) D -= a.c_kl * e;
+        const float d = (float)((double)in.ref - lp), e = expm1f(d);
+        sum[3] += w * (double)divergence(d, e);
+        if (a.c_kl != 0.0) D -= a.c_kl * (double)e;
     }
     if (clipped) sum[4] += w;
     return make_float2((float)(w * D), (float)(w * a.c_entropy));
 }
 
-// Sums of the waves of a block into the block's place; blocks are joined by policy_terms_kernel.
+// Terms of the loss from the sums over all decisions.
+__device__ __forceinline__ void write_terms(const PolicyArgs &a, const double *v)
+{
+    double total = v[0];
+    if (a.c_value != 0.0) total += a.c_value * v[1];
+    if (a.c_entropy != 0.0) total -= a.c_entropy * v[2];
+    if (a.c_kl != 0.0) total += a.c_kl * v[3];
+    a.terms[0] = (float)total;
+    for (int i = 0; i < kPolicySums; ++i) a.terms[1 + i] = (float)v[i];
+}
+
+// A block's sums, from n partial ones in LDS, to the block's place, where policy_terms_kernel joins them; the only block of a launch writes the
+// terms itself.  Ends without a barrier.
+__device__ __forceinline__ void store_partials(const PolicyArgs &a, const double (*lds)[kPolicySums], int n)
+{
+    if (threadIdx.x != 0) return;
+    double v[kPolicySums];
+#pragma unroll
+    for (int i = 0; i < kPolicySums; ++i) {
+        v[i] = 0.0;
+        for (int w = 0; w < n; ++w) v[i] += lds[w][i];
+    }
+    if (gridDim.x == 1) {
+        write_terms(a, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPolicySums; ++i) a.sums[(int64_t)blockIdx.x * kPolicySums + i] = v[i];
+    }
+}
+
 template <int WAVES>
 __device__ __forceinline__ void store_sums(const PolicyArgs &a, const double (&sum)[kPolicySums])
 {
@@ -122,11 +274,7 @@ __device__ __forceinline__ void store_sums(const PolicyArgs &a, const double (&s
         if (lane == 0) lds[wave][i] = v;
     }
     __syncthreads();
-    if (threadIdx.x < kPolicySums) {
-        double v = 0.0;
-        for (int w = 0; w < WAVES; ++w) v += lds[w][threadIdx.x];
-        a.sums[(int64_t)blockIdx.x * kPolicySums + threadIdx.x] = v;
-    }
+    store_partials(a, lds, WAVES);
 }
 
 // Terms from the blocks' sums, in a fixed order.  Zeros where there are no blocks.
@@ -147,13 +295,8 @@ __global__ void __launch_bounds__(kThreads) policy_terms_kernel(const PolicyArgs
         for (int i = 0; i < kPolicySums; ++i) {
             v[i] = 0.0;
             for (int w = 0; w < kThreads / 64; ++w) v[i] += lds[w][i];
-            a.terms[1 + i] = (float)v[i];
         }
-        double total = v[0];
-        if (a.c_value != 0.0) total += a.c_value * v[1];
-        if (a.c_entropy != 0.0) total -= a.c_entropy * v[2];
-        if (a.c_kl != 0.0) total += a.c_kl * v[3];
-        a.terms[0] = (float)total;
+        write_terms(a, v);
     }
 }
 
@@ -232,12 +375,14 @@ __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs 
             for (int i = tid; i < items; i += kThreads) x[at(i)] = T::get(logits[offset(i, a.ld_r, a.ld_g)]);
         __syncthreads();
 
-        float m[kHeadsPerThread], ls[kHeadsPerThread], ent[kHeadsPerThread];
+        Soft v[kHeadsPerThread];
+        float2 le[kHeadsPerThread];
         int c[kHeadsPerThread];
 #pragma unroll
         for (int u = 0; u < kHeadsPerThread; ++u) {
             const int h = tid + u * kThreads;
-            m[u] = ls[u] = ent[u] = 0.0f;
+            v[u] = soft_none();
+            le[u] = make_float2(0.0f, 0.0f);
             c[u] = -1;
             if (h >= heads) continue;
             const float *xh = x + h * k.stride;
@@ -245,21 +390,19 @@ __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs 
             float lp = 0.0f;
             if (c[u] == a.V) {
                 c[u] = 0;
-                ls[u] = ent[u] = lp = __builtin_nanf("");
+                le[u].x = le[u].y = v[u].s = lp = __builtin_nanf("");
             } else if (c[u] >= 0) {
-                Soft v = soft_none();
-                for (int j = 0; j < a.V; ++j) v.m = fmaxf(v.m, xh[j]);
-                for (int j = 0; j < a.V; ++j) soft_add(v, xh[j]);
-                if (v.s != 0.0f) {
-                    m[u] = v.m;
-                    ls[u] = logf(v.s);
-                    ent[u] = ls[u] - v.t / v.s;
-                    lp = xh[c[u]] - v.m - ls[u];
+                for (int j = 0; j < a.V; ++j) v[u].m = fmaxf(v[u].m, xh[j]);
+                const Scale k2 = scale_of(v[u].m);
+                for (int j = 0; j < a.V; ++j) soft_add(v[u], xh[j], k2);
+                if (v[u].s != 0.0f) {
+                    le[u] = log_and_entropy(v[u]);
+                    lp = xh[c[u]] - v[u].m - le[u].x;
                 } else {
                     c[u] = -1;                  // every choice is masked
                 }
             }
-            one[h] = make_float2(lp, ent[u]);
+            one[h] = make_float2(lp, le[u].y);
             in[h] = c[u] >= 0;
         }
         __syncthreads();
@@ -273,7 +416,7 @@ __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs 
                     H += (double)o.y;
                     any = any || in[r * a.G + g] != 0;
                 }
-            dec[r] = decide(a, r0 + r, any, lp, H, sum);
+            dec[r] = decide(a, r0 + r, given_of(a, r0 + r, load_plain), any, lp, H, sum);
             if (!any)                           // also of weight 0: zeros, whatever the logits are
                 for (int g = 0; g < a.G; ++g) in[r * a.G + g] = 0;
         }
@@ -292,10 +435,9 @@ __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs 
                 continue;
             }
             const float2 d = dec[a.G == 1 ? h : h / a.G];
-            for (int j = 0; j < a.V; ++j) {
-                const float z = xh[j] - m[u] - ls[u], p = exp_fast(z);
-                xh[j] = (j == c[u] ? d.x : 0.0f) - p * (d.x - d.y * (fmaxf(z, kFar) + ent[u]));
-            }
+            const Slope f = slope_of(v[u].m, v[u].s, le[u].x, le[u].y, d);
+            for (int j = 0; j < a.V; ++j) xh[j] = slope_at<true>(f, xh[j]);
+            xh[c[u]] += d.x;
         }
         __syncthreads();
         typename T::item *grad = static_cast<typename T::item *>(a.grad);
@@ -308,25 +450,177 @@ __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs 
     if (a.old_logp) store_sums<kThreads / 64>(a, sum);
 }
 
-// --- any number of heads and choices, in three steps: sums of parts of heads, decisions, gradient
+// --- one head of more choices: a row stays in the registers of a wave or a workgroup between its sums and its gradient
 
-// Visits the items [lo, hi) of a row, 16 bytes at a time from the first boundary on; f(index, value).
-template <typename T, typename F>
-__device__ __forceinline__ void for_items(const typename T::item *row, int lo, int hi, F &&f)
+// Waves of a SIMD that the registers of N pieces a thread leave room for.
+constexpr int row_waves(int n) { return n >= 16 ? 4 : n >= 8 ? 5 : 6; }
+
+template <typename T>
+__device__ __forceinline__ uint4 masked_items()          // 16 bytes of -inf
 {
-    const int head = (int)items_to_boundary<T>(row + lo, hi - lo);
-    const int n_vec = (hi - lo - head) / T::kVec;
-    if ((int)threadIdx.x < head) f(lo + (int)threadIdx.x, T::get(row[lo + threadIdx.x]));
-    const uint4 *body = reinterpret_cast<const uint4 *>(row + lo + head);
-    for (int i = threadIdx.x; i < n_vec; i += kThreads) {
-        float x[T::kVec];
-        T::unpack(body[i], x);
-#pragma unroll
-        for (int j = 0; j < T::kVec; ++j) f(lo + head + i * T::kVec + j, x[j]);
-    }
-    const int tail = lo + head + n_vec * T::kVec;
-    if ((int)threadIdx.x < hi - tail) f(tail + (int)threadIdx.x, T::get(row[tail + threadIdx.x]));
+    const uint32_t w = sizeof(typename T::item) == 4 ? 0xff800000u : T::kMasked * 0x10001u;
+    return make_uint4(w, w, w, w);
 }
+
+// Unpacked items are not carried from one use to the next: they would take twice the registers.
+__device__ __forceinline__ void keep_packed(uint4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
+
+// Sums of a thread's items joined over the THREADS of a row; every thread returns the row's.
+template <int THREADS>
+__device__ __forceinline__ Soft soft_row(Soft v, Soft *lds)
+{
+    v = soft_wave(v);
+    if (THREADS == 64) return v;
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float m = kLowest, sum = 0.0f, t = 0.0f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) m = fmaxf(m, lds[w].m);
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        Soft o = lds[w];
+        soft_raise(o, m);
+        sum += o.s;
+        t += o.t;
+    }
+    return {m, sum, t};
+}
+
+// A gradient is not read again here: it goes past the caches, which then hold what rows longer than the registers are read from a second time
+// (fp32 4096 x 50021 398 -> 355 us, 1024 x 131072 311 -> 256, bf16 4096 x 131072 533 -> 508).
+// Its 16 bytes may begin at any item: the hardware takes that, only slower.
+template <typename T>
+__device__ __forceinline__ void store_past(typename T::item *p, const uint4 &v)
+{
+    const typename T::words w = {v.x, v.y, v.z, v.w};
+    __builtin_nontemporal_store(w, reinterpret_cast<typename T::words *>(p));
+}
+
+// Where the items of a decision's row stand: an unaligned head and tail around pieces of 16 bytes.
+struct RowAt {
+    int choice;                                          // of its action; -1: left out
+    int head, n_vec, tail;
+};
+
+// THREADS of a row hold N x 16 bytes of it each, and its ends up to the first and from the last 16-byte boundary an item each; what is left of
+// longer rows is read once for the sums and once for the gradient.  A workgroup stays, and asks for a piece of its next row as
+// soon as it is done with that of the present one, so that loads are under way while sums are joined and gradients stored.
+template <typename T, int THREADS, int N, bool GRAD, bool ENT>
+__global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_waves(N)) policy_row_kernel(const PolicyArgs a)
+{
+    constexpr int kBlock = THREADS < kThreads ? kThreads : THREADS, kRows = kBlock / THREADS;
+    __shared__ Soft lds[THREADS / 64];
+    __shared__ float2 dec;
+    __shared__ double sum[kRows][kPolicySums];           // of the rows of a group so far, by its first thread
+    const int tid = threadIdx.x % THREADS, group = THREADS == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
+    if (tid < kPolicySums) sum[group][tid] = 0.0;
+    __syncthreads();
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    const auto row_of = [&](int64_t r) { return static_cast<const typename T::item *>(a.logits) + r * a.ld_r; };
+    const auto look_up = [&](int64_t r) {
+        RowAt at{-1, 0, 0, 0};
+        if (r < a.R) {
+            at.choice = counts(a, r) ? choice_of(a, r) : -1;
+            at.head = (int)items_to_boundary<T>(row_of(r), a.V);
+            at.n_vec = (a.V - at.head) / T::kVec;
+            at.tail = a.V - at.head - at.n_vec * T::kVec;
+        }
+        return at;
+    };
+    uint4 held[N];
+    const auto ask = [&](int64_t r, const RowAt &at, int k) {
+        const uint4 *body = reinterpret_cast<const uint4 *>(row_of(r) + at.head);
+        held[k] = masked_items<T>();
+        if (at.choice >= 0 && tid + k * THREADS < at.n_vec) held[k] = body[tid + k * THREADS];
+    };
+    int64_t r = (int64_t)blockIdx.x * kRows + group;
+    RowAt now = look_up(r);
+#pragma unroll
+    for (int k = 0; k < N; ++k) ask(r, now, k);
+    for (; r < a.R; r += step) {
+        const typename T::item *row = row_of(r);
+        typename T::item *to = GRAD ? static_cast<typename T::item *>(a.grad) + r * a.gld_r : nullptr;
+        const int c = now.choice, head = now.head, n_vec = now.n_vec;
+        const uint4 *body = reinterpret_cast<const uint4 *>(row + head);
+        const int end_at = tid < head ? tid : tid < head + now.tail ? n_vec * T::kVec + tid : -1;
+        float end[1] = {-__builtin_inff()}, xa = 0.0f;
+        if (c >= 0 && end_at >= 0) end[0] = T::get(row[end_at]);
+        if (c >= 0 && c < a.V) xa = T::get(row[c]);      // before a gradient in place
+        const RowAt next = look_up(r + step);
+        const Given given = given_of(a, r, load_shared);
+        Soft v = soft_none();
+        if (c >= 0) {
+            Scale k2 = scale_of(v.m);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                if (k * THREADS < n_vec) {               // of all threads
+                    float x[T::kVec];
+                    T::unpack(held[k], x);
+                    soft_add_all(v, k2, x);
+                }
+                if (!GRAD) ask(r + step, next, k);
+                else keep_packed(held[k]);
+            }
+            for (int i = tid + N * THREADS; i < n_vec; i += THREADS) {
+                float x[T::kVec];
+                T::unpack(body[i], x);
+                soft_add_all(v, k2, x);
+            }
+            soft_add_all(v, k2, end);
+        } else if (!GRAD) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) ask(r + step, next, k);
+        }
+        v = soft_row<THREADS>(v, lds);
+        bool in = c >= 0 && v.s != 0.0f;                 // 0: every choice is masked
+        if (c == a.V) {
+            in = true;
+            v.s = __builtin_nanf("");
+        }
+        const float2 le = log_and_entropy(v);
+        float2 d = make_float2(0.0f, 0.0f);
+        if (tid == 0) d = decide(a, r, given, in, in ? (double)xa - (double)v.m - (double)le.x : 0.0, in ? (double)le.y : 0.0, sum[group]);
+        if (THREADS == 64) {
+            d.x = readlane_f(d.x, 0);
+            d.y = readlane_f(d.y, 0);
+        } else {
+            if (tid == 0) dec = d;
+            __syncthreads();                             // lds is written again, too
+            d = dec;
+        }
+        if (GRAD) {
+            const Slope f = slope_of(v.m, v.s, le.x, le.y, d);
+            auto write = [&](int i, const uint4 &raw) {
+                float x[T::kVec];
+                T::unpack(raw, x);
+#pragma unroll
+                for (int j = 0; j < T::kVec; ++j) x[j] = slope_at<ENT>(f, x[j]);
+                store_past<T>(to + head + i * T::kVec, T::pack(x));
+            };
+            // the next row's pieces are asked for as this one's registers come free
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                if (in && tid + k * THREADS < n_vec) write(tid + k * THREADS, held[k]);
+                ask(r + step, next, k);
+            }
+            if (in) {
+                for (int i = tid + N * THREADS; i < n_vec; i += THREADS) write(i, body[i]);
+                if (end_at >= 0) to[end_at] = T::put(slope_at<ENT>(f, end[0]));
+                // the action's item once more, by the thread that has written it
+                const bool owner = c < head || c >= head + n_vec * T::kVec ? end_at == c : (c - head) / T::kVec % THREADS == tid;
+                if (owner && c < a.V) to[c] = T::put(slope_at<ENT>(f, xa) + d.x);
+            } else {
+                for (int i = tid; i < n_vec; i += THREADS) store_past<T>(to + head + i * T::kVec, make_uint4(0, 0, 0, 0));
+                if (end_at >= 0) to[end_at] = T::put(0.0f);
+            }
+        }
+        now = next;
+    }
+    __syncthreads();
+    if (a.old_logp) store_partials(a, sum, kRows);
+}
+
+// --- any number of heads and choices, in three steps: sums of parts of heads, decisions, gradient
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) policy_part_kernel(const PolicyArgs a, int splits, int chunk)
@@ -342,10 +636,18 @@ __global__ void __launch_bounds__(kThreads) policy_part_kernel(const PolicyArgs 
         const int hi = lo + chunk < a.V ? lo + chunk : a.V;
         const typename T::item *row = static_cast<const typename T::item *>(a.logits) + r * a.ld_r + g * a.ld_g;
         Soft v = soft_none();
-        for_items<T>(row, lo, hi, [&](int, float x) {
-            soft_raise(v, x);
-            soft_add(v, x);
-        });
+        const int head = (int)items_to_boundary<T>(row + lo, hi - lo), n_vec = (hi - lo - head) / T::kVec, tail = lo + head + n_vec * T::kVec;
+        const uint4 *body = reinterpret_cast<const uint4 *>(row + lo + head);
+        float end[2] = {-__builtin_inff(), -__builtin_inff()};
+        if ((int)threadIdx.x < head) end[0] = T::get(row[lo + threadIdx.x]);
+        if ((int)threadIdx.x < hi - tail) end[1] = T::get(row[tail + threadIdx.x]);
+        Scale k2 = scale_of(v.m);
+        soft_add_all(v, k2, end);
+        for (int i = threadIdx.x; i < n_vec; i += kThreads) {
+            float x[T::kVec];
+            T::unpack(body[i], x);
+            soft_add_all(v, k2, x);
+        }
         v = soft_wave(v);
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
         __syncthreads();
@@ -358,12 +660,12 @@ __global__ void __launch_bounds__(kThreads) policy_part_kernel(const PolicyArgs 
 }
 
 // A wave per decision: its heads one after the other, the parts of a head over the lanes.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) policy_join_kernel(const PolicyArgs a, int splits)
+template <typename T, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) policy_join_kernel(const PolicyArgs a, int splits)
 {
     const int lane = threadIdx.x & 63;
     double sum[kPolicySums] = {};
-    for (int64_t r = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); r < a.R; r += (int64_t)gridDim.x * (kThreads / 64)) {
+    for (int64_t r = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6); r < a.R; r += (int64_t)gridDim.x * WAVES) {
         double lp = 0.0, H = 0.0;
         bool in = false;
         if (counts(a, r)) {
@@ -383,11 +685,11 @@ __global__ void __launch_bounds__(kThreads) policy_join_kernel(const PolicyArgs 
                     }
                     v = soft_wave(v);
                     if (v.s != 0.0f) {                     // 0: every choice is masked
-                        const float ls = logf(v.s), e = ls - v.t / v.s;
+                        const float2 le = log_and_entropy(v);
                         const float x = T::get(static_cast<const typename T::item *>(a.logits)[r * a.ld_r + g * a.ld_g + c]);
-                        lp += (double)x - (double)v.m - (double)ls;
-                        H += (double)e;
-                        out = make_float4(v.m, ls, e, __int_as_float(c));
+                        lp += (double)x - (double)v.m - (double)le.x;
+                        H += (double)le.y;
+                        out = make_float4(v.m, v.s, le.y, __int_as_float(c));
                         in = true;
                     }
                 }
@@ -395,11 +697,11 @@ __global__ void __launch_bounds__(kThreads) policy_join_kernel(const PolicyArgs 
             }
         }
         if (lane == 0) {
-            const float2 d = decide(a, r, in, lp, H, sum);
+            const float2 d = decide(a, r, given_of(a, r, load_plain), in, lp, H, sum);
             if (a.grad) a.dec[r] = d;
         }
     }
-    if (a.old_logp) store_sums<kThreads / 64>(a, sum);
+    if (a.old_logp) store_sums<WAVES>(a, sum);
 }
 
 template <typename T>
@@ -419,19 +721,75 @@ __global__ void __launch_bounds__(kThreads) policy_grad_kernel(const PolicyArgs 
         }
         const float2 d = a.dec[r];
         const typename T::item *row = static_cast<const typename T::item *>(a.logits) + r * a.ld_r + g * a.ld_g;
-        for_items<T>(row, lo, hi, [&](int v, float x) {
-            const float z = x - k.x - k.y, p = exp_fast(z);
-            to[v] = T::put((v == c ? d.x : 0.0f) - p * (d.x - d.y * (fmaxf(z, kFar) + k.z)));
-        });
+        const Slope f = slope_of(k.x, k.y, logf(k.y), k.z, d);
+        const int head = (int)items_to_boundary<T>(row + lo, hi - lo), n_vec = (hi - lo - head) / T::kVec, tail = lo + head + n_vec * T::kVec;
+        auto one = [&](int v) { to[v] = T::put(slope_at<true>(f, T::get(row[v])) + (v == c ? d.x : 0.0f)); };
+        if ((int)threadIdx.x < head) one(lo + threadIdx.x);
+        if ((int)threadIdx.x < hi - tail) one(tail + threadIdx.x);
+        for (int i = threadIdx.x; i < n_vec; i += kThreads) {
+            const int at = lo + head + i * T::kVec;
+            float x[T::kVec];
+            T::unpack(*reinterpret_cast<const uint4 *>(row + at), x);
+#pragma unroll
+            for (int j = 0; j < T::kVec; ++j) x[j] = slope_at<true>(f, x[j]) + (at + j == c ? d.x : 0.0f);
+            store_past<T>(to + at, T::pack(x));
+        }
     }
 }
 
 constexpr int kJoinBlocks = 1024;
 constexpr int kTileBlocks = 1024;               // what is on the chip at a time
+constexpr int kUnits = 256;                     // compute units
+constexpr int kRowBlocks = 6 * kUnits;
+constexpr int kJoinFew = 16;                    // decisions that one workgroup joins, a wave each
+
+// A wave or a workgroup per row, by its pieces of 16 bytes: 64 threads up to 1024 pieces (four rows a workgroup, no barrier), 256 up to
+// 4096, 512 beyond, up to sixteen pieces a thread.  us a loss, bf16, 64 / 256 threads: 6001 x 8191 42 / 49, 16384 x 4096 64 / 81; 256 / 512:
+// 8192 x 32768 (256 / 1024) 229 / 286, 4096 x 65536 249 / 236; 512 / 1024: 4096 x 65536 236 / 272, 4096 x 131072 510 / 497, fp32 1024 x 131072 255 / 244.
+// Fewer rows than what fills the chip take the next size, as a row is then all latency: 512 x 8192 15.0 / 11.5, 1024 x 8192
+// 17.0 / 16.6, 1024 x 4096 12.1 / 12.9; fp32 256 x 16384 (4096 pieces; 256 / 1024) 15.6 / 14.3, bf16 (2048 pieces) 12.1 / 12.5.
+// Beyond 4096 pieces log-probabilities alone take a row in parts, which a workgroup reads without holding it (bf16 4096 x 131072,
+// row / parts, 245 / 194 us, fp32 1024 x 50021 40 / 36; at 4096 pieces, 2048 x 32768, 26 / 28), and gradients do so for few rows:
+// the row is read twice, but by many workgroups: 9 x 131072 bf16 24 / 15, 64 26 / 23, 128 30 / 31; fp32 32 x 50021 19 / 17, 128 23 / 26.
+constexpr int kWideRow = 4096;
+constexpr int kFewRows = 1024, kVeryFewRows = 256;
 constexpr unsigned kMostBlocks = 1u << 20;
 
 unsigned blocks_for(int64_t n) { return (unsigned)(n < (int64_t)kMostBlocks ? n : (int64_t)kMostBlocks); }
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
+
+// The terms of a loss, unless its only workgroup has written them.
+hipError_t launch_terms(const PolicyArgs &a, unsigned blocks, hipStream_t s)
+{
+    if (a.old_logp && (a.R == 0 || blocks > 1))
+        hipLaunchKernelGGL(policy_terms_kernel, dim3(1), dim3(kThreads), 0, s, a, a.R > 0 ? (int)blocks : 0);
+    return hipGetLastError();
+}
+
+template <typename T, int THREADS, int N>
+void launch_row_of(const PolicyArgs &a, unsigned blocks, hipStream_t s)
+{
+    const dim3 block(THREADS < kThreads ? kThreads : THREADS);
+    if (!a.grad) hipLaunchKernelGGL((policy_row_kernel<T, THREADS, (N < 8 ? N : 8), false, false>), dim3(blocks), block, 0, s, a);
+    else if (a.c_entropy != 0.0) hipLaunchKernelGGL((policy_row_kernel<T, THREADS, N, true, true>), dim3(blocks), block, 0, s, a);
+    else hipLaunchKernelGGL((policy_row_kernel<T, THREADS, N, true, false>), dim3(blocks), block, 0, s, a);
+}
+template <typename T>
+void launch_row(const PolicyArgs &a, const PolicyPlan &p, unsigned blocks, hipStream_t s)
+{
+    switch (p.threads + p.row) {
+    case 64 + 1: return launch_row_of<T, 64, 1>(a, blocks, s);
+    case 64 + 2: return launch_row_of<T, 64, 2>(a, blocks, s);
+    case 64 + 4: return launch_row_of<T, 64, 4>(a, blocks, s);
+    case 64 + 8: return launch_row_of<T, 64, 8>(a, blocks, s);
+    case 64 + 16: return launch_row_of<T, 64, 16>(a, blocks, s);
+    case 256 + 4: return launch_row_of<T, 256, 4>(a, blocks, s);
+    case 256 + 8: return launch_row_of<T, 256, 8>(a, blocks, s);
+    case 256 + 16: return launch_row_of<T, 256, 16>(a, blocks, s);
+    case 512 + 8: return launch_row_of<T, 512, 8>(a, blocks, s);
+    default: return launch_row_of<T, 512, 16>(a, blocks, s);
+    }
+}
 
 template <typename T>
 hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
@@ -448,18 +806,25 @@ hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
         const int64_t tiles = (a.R + p.tile - 1) / p.tile;
         const unsigned blocks = (unsigned)(tiles < kTileBlocks ? tiles : kTileBlocks);
         if (a.R > 0) hipLaunchKernelGGL(policy_tile_kernel<T>, dim3(blocks), dim3(kThreads), 0, s, a, k);
-        if (a.old_logp) hipLaunchKernelGGL(policy_terms_kernel, dim3(1), dim3(kThreads), 0, s, a, (int)blocks);
-        return hipGetLastError();
+        return launch_terms(a, blocks, s);
+    }
+    if (p.row) {
+        const int rows = p.threads < kThreads ? kThreads / p.threads : 1;
+        const int64_t groups = (a.R + rows - 1) / rows;
+        const int64_t resident = (int64_t)kUnits * (row_waves(p.row) * 4 / (p.threads < kThreads ? kThreads / 64 : p.threads / 64));
+        const unsigned blocks = (unsigned)(groups < resident ? groups : resident);
+        if (a.R > 0) launch_row<T>(a, p, blocks, s);
+        return launch_terms(a, blocks, s);
     }
     const int64_t units = a.R * a.G * p.splits;
-    const unsigned join = (unsigned)((a.R + 3) / 4 < kJoinBlocks ? (a.R + 3) / 4 : kJoinBlocks);
+    const unsigned join = (unsigned)(a.R <= kJoinFew ? 1 : (a.R + 3) / 4 < kJoinBlocks ? (a.R + 3) / 4 : kJoinBlocks);
     if (a.R > 0) {
         hipLaunchKernelGGL(policy_part_kernel<T>, dim3(blocks_for(units)), dim3(kThreads), 0, s, a, p.splits, p.chunk);
-        hipLaunchKernelGGL(policy_join_kernel<T>, dim3(join), dim3(kThreads), 0, s, a, p.splits);
+        if (join == 1) hipLaunchKernelGGL((policy_join_kernel<T, kJoinFew>), dim3(1), dim3(kJoinFew * 64), 0, s, a, p.splits);
+        else hipLaunchKernelGGL((policy_join_kernel<T, kThreads / 64>), dim3(join), dim3(kThreads), 0, s, a, p.splits);
         if (a.grad) hipLaunchKernelGGL(policy_grad_kernel<T>, dim3(blocks_for(units)), dim3(kThreads), 0, s, a, p.splits, p.chunk);
     }
-    if (a.old_logp) hipLaunchKernelGGL(policy_terms_kernel, dim3(1), dim3(kThreads), 0, s, a, (int)join);
-    return hipGetLastError();
+    return launch_terms(a, join, s);
 }
 
 }  // namespace
@@ -471,6 +836,18 @@ PolicyPlan plan_policy(int64_t R, int G, int V, int type, bool grad)
         const int by_heads = kTileHeads / G, by_items = kTileItems / (G * (V | 1));
         p.tile = by_heads < by_items ? by_heads : by_items;
         p.bytes = (int64_t)kTileBlocks * kPolicySums * 8;
+        return p;
+    }
+    const int vecs = V / (16 / type_bytes(type));
+    if (G == 1 && (vecs <= kWideRow || (grad && R * 256 > vecs))) {
+        p.threads = vecs <= 1024 ? 64 : vecs <= kWideRow ? 256 : 512;
+        if (R < kFewRows && vecs > 256 && vecs <= 1024) p.threads = 256;
+        if (R <= kVeryFewRows && vecs > 2048) p.threads = 512;
+        const int n = (vecs + p.threads - 1) / p.threads;
+        p.row = n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : n <= 8 ? 8 : 16;
+        if (p.threads == 256 && p.row < 4) p.row = 4;
+        if (p.threads == 512 && p.row < 8) p.row = 8;
+        p.bytes = (int64_t)kRowBlocks * kPolicySums * 8;
         return p;
     }
     // parts of a head: of at least 4096 choices, until there are 1024 workgroups
