@@ -11,10 +11,11 @@ namespace cham {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kChunk = 1 << 14;            // items of a chunk: a workgroup takes one at a time
+constexpr int kThreads = 512;
+constexpr int kPieces = 4;                 // of 16 bytes that a thread asks for at a time
+constexpr int kChunkBytes = kThreads * kPieces * 16;
 constexpr int kMostTensors = 120;          // of a launch: 4 KiB of arguments
-constexpr int kBlocks = 1024;              // workgroups of all launches of a call together, but one each at least
+constexpr int kBlocks = 1024;              // workgroups of all launches of a call together (what is on the chip at a time), but one each at least
 
 struct Tensors {
     const void *from[kMostTensors];
@@ -52,44 +53,80 @@ __device__ __forceinline__ double block_sum(double v)
     return s;
 }
 
+// A chunk's 16-byte pieces may begin at any item: the hardware takes that, and no sum depends on where a tensor lies.
 template <typename T>
-__device__ __forceinline__ double chunk_squares(const void *from, int n)
+__device__ __forceinline__ uint4 piece(const typename T::item *p, int i)
 {
-    const typename T::item *p = static_cast<const typename T::item *>(from);
-    const int head = (int)items_to_boundary<T>(p, n), n_vec = (n - head) / T::kVec, tail = head + n_vec * T::kVec;
-    const uint4 *body = reinterpret_cast<const uint4 *>(p + head);
-    double s = 0.0;
-    if ((int)threadIdx.x < head) {
-        const double x = (double)T::get(p[threadIdx.x]);
-        s += x * x;
-    }
-    if ((int)threadIdx.x < n - tail) {
-        const double x = (double)T::get(p[tail + threadIdx.x]);
-        s += x * x;
-    }
-    for (int i = threadIdx.x; i < n_vec; i += kThreads) {
-        float x[T::kVec];
-        T::unpack(body[i], x);
-#pragma unroll
-        for (int j = 0; j < T::kVec; ++j) s = __builtin_fma((double)x[j], (double)x[j], s);
-    }
-    return s;
+    const typename T::words w = *reinterpret_cast<const typename T::words *>(p + i * T::kVec);
+    return make_uint4(w.x, w.y, w.z, w.w);
 }
 
-__global__ void __launch_bounds__(kThreads) grad_squares_kernel(const Tensors t, double *parts)
+template <typename T>
+__device__ __forceinline__ void add_squares(const uint4 &raw, double (&s)[4])
 {
-    double s = 0.0;
-    for (int c = (int)blockIdx.x; c < t.first[t.n]; c += (int)gridDim.x) {
-        const int i = tensor_of(t, c);
-        const int64_t at = (int64_t)(c - t.first[i]) * kChunk;
-        const int64_t left = t.numel[i] - at;
-        const int n = left < kChunk ? (int)left : kChunk;
-        if (t.type[i] == 0) s += chunk_squares<F32>(static_cast<const float *>(t.from[i]) + at, n);
-        else if (t.type[i] == 1) s += chunk_squares<BF16>(static_cast<const __bf16 *>(t.from[i]) + at, n);
-        else s += chunk_squares<F16>(static_cast<const _Float16 *>(t.from[i]) + at, n);
+    float x[T::kVec];
+    T::unpack(raw, x);
+#pragma unroll
+    for (int j = 0; j < T::kVec; ++j) s[j % 4] = __builtin_fma((double)x[j], (double)x[j], s[j % 4]);
+}
+
+template <typename T>
+__device__ __forceinline__ void chunk_squares(const void *from, int n, double (&s)[4])
+{
+    const typename T::item *p = static_cast<const typename T::item *>(from);
+    const int tid = threadIdx.x, n_vec = n / T::kVec;
+    uint4 held[kPieces];
+    if (n_vec == kThreads * kPieces) {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) held[k] = piece<T>(p, tid + k * kThreads);
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) add_squares<T>(held[k], s);
+        return;
     }
-    s = block_sum(s);
-    if (threadIdx.x == 0) parts[blockIdx.x] = s;
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+        held[k] = make_uint4(0, 0, 0, 0);
+        if (tid + k * kThreads < n_vec) held[k] = piece<T>(p, tid + k * kThreads);
+    }
+    double x = 0.0;
+    if (tid < n - n_vec * T::kVec) x = (double)T::get(p[n_vec * T::kVec + tid]);
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) add_squares<T>(held[k], s);
+    s[0] = __builtin_fma(x, x, s[0]);
+}
+
+// The chunks [lo, hi) of a block: consecutive ones, so that a tensor is looked up once and then followed.
+__device__ __forceinline__ void share_of(const Tensors &t, int &lo, int &hi)
+{
+    const int64_t n = t.first[t.n];
+    lo = (int)(n * blockIdx.x / gridDim.x);
+    hi = (int)(n * (blockIdx.x + 1) / gridDim.x);
+}
+
+struct Chunk {
+    int64_t at;                            // first item
+    int n;
+};
+__device__ __forceinline__ Chunk chunk_of(const Tensors &t, int tensor, int chunk)
+{
+    const int64_t items = kChunkBytes / (t.type[tensor] == 0 ? 4 : 2), at = (chunk - t.first[tensor]) * items, left = t.numel[tensor] - at;
+    return {at, (int)(left < items ? left : items)};
+}
+
+__global__ void __launch_bounds__(kThreads, 8) grad_squares_kernel(const Tensors t, double *parts)
+{
+    double s[4] = {};
+    int lo, hi;
+    share_of(t, lo, hi);
+    for (int c = lo, i = tensor_of(t, lo); c < hi; ++c) {
+        while (c >= t.first[i + 1]) ++i;
+        const Chunk k = chunk_of(t, i, c);
+        if (t.type[i] == 0) chunk_squares<F32>(static_cast<const float *>(t.from[i]) + k.at, k.n, s);
+        else if (t.type[i] == 1) chunk_squares<BF16>(static_cast<const __bf16 *>(t.from[i]) + k.at, k.n, s);
+        else chunk_squares<F16>(static_cast<const _Float16 *>(t.from[i]) + k.at, k.n, s);
+    }
+    const double sum = block_sum((s[0] + s[1]) + (s[2] + s[3]));
+    if (threadIdx.x == 0) parts[blockIdx.x] = sum;
 }
 
 __device__ __forceinline__ double norm_of(const double *parts, int n_parts)
@@ -106,30 +143,36 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double *parts
 }
 
 template <typename T>
+__device__ __forceinline__ void scale_piece(typename T::item *q, int i, const uint4 &raw, float f)
+{
+    float x[T::kVec];
+    T::unpack(raw, x);
+#pragma unroll
+    for (int j = 0; j < T::kVec; ++j) x[j] *= f;
+    const uint4 v = T::pack(x);
+    const typename T::words w = {v.x, v.y, v.z, v.w};
+    __builtin_nontemporal_store(w, reinterpret_cast<typename T::words *>(q + i * T::kVec));
+}
+template <typename T>
 __device__ __forceinline__ void chunk_scale(const void *from, void *to, int n, float f)
 {
     const typename T::item *p = static_cast<const typename T::item *>(from);
     typename T::item *q = static_cast<typename T::item *>(to);
-    if (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15) != 0) {      // boundaries at different items
-        for (int i = threadIdx.x; i < n; i += kThreads) q[i] = T::put(T::get(p[i]) * f);
-        return;
-    }
-    const int head = (int)items_to_boundary<T>(p, n), n_vec = (n - head) / T::kVec, tail = head + n_vec * T::kVec;
-    const uint4 *body = reinterpret_cast<const uint4 *>(p + head);
-    uint4 *out = reinterpret_cast<uint4 *>(q + head);
-    if ((int)threadIdx.x < head) q[threadIdx.x] = T::put(T::get(p[threadIdx.x]) * f);
-    if ((int)threadIdx.x < n - tail) q[tail + threadIdx.x] = T::put(T::get(p[tail + threadIdx.x]) * f);
-    for (int i = threadIdx.x; i < n_vec; i += kThreads) {
-        float x[T::kVec];
-        T::unpack(body[i], x);
+    const int tid = threadIdx.x, n_vec = n / T::kVec, at = n_vec * T::kVec + tid;
+    uint4 held[kPieces];
 #pragma unroll
-        for (int j = 0; j < T::kVec; ++j) x[j] *= f;
-        out[i] = T::pack(x);
-    }
+    for (int k = 0; k < kPieces; ++k)
+        if (tid + k * kThreads < n_vec) held[k] = piece<T>(p, tid + k * kThreads);
+    typename T::item last{};
+    if (at < n) last = p[at];
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+        if (tid + k * kThreads < n_vec) scale_piece<T>(q, tid + k * kThreads, held[k], f);
+    if (at < n) q[at] = T::put(T::get(last) * f);
 }
 
 // parts: the sums of squares of this call (block 0 of the first launch notes the norm); null: *norm is given.
-__global__ void __launch_bounds__(kThreads) grad_clip_kernel(const Tensors t, double max_norm, const double *parts, int n_parts, double *norm, int first)
+__global__ void __launch_bounds__(kThreads, 8) grad_clip_kernel(const Tensors t, double max_norm, const double *parts, int n_parts, double *norm, int first)
 {
     double v;
     if (parts) {
@@ -140,17 +183,23 @@ __global__ void __launch_bounds__(kThreads) grad_clip_kernel(const Tensors t, do
     }
     const bool whole = v + 1e-6 <= max_norm;
     const float f = whole ? 1.0f : (float)(max_norm / (v + 1e-6));
+    int lo, hi;
+    share_of(t, lo, hi);
     // from the last chunk to the first: what the sum of squares has read last is still in cache
-    for (int c = t.first[t.n] - 1 - (int)blockIdx.x; c >= 0; c -= (int)gridDim.x) {
-        const int i = tensor_of(t, c);
+    for (int c = hi - 1, i = lo < hi ? tensor_of(t, hi - 1) : 0; c >= lo; --c) {
+        while (c < t.first[i]) --i;
         if (whole && t.from[i] == t.to[i]) continue;
-        const int64_t at = (int64_t)(c - t.first[i]) * kChunk;
-        const int64_t left = t.numel[i] - at;
-        const int n = left < kChunk ? (int)left : kChunk;
-        if (t.type[i] == 0) chunk_scale<F32>(static_cast<const float *>(t.from[i]) + at, static_cast<float *>(t.to[i]) + at, n, f);
-        else if (t.type[i] == 1) chunk_scale<BF16>(static_cast<const __bf16 *>(t.from[i]) + at, static_cast<__bf16 *>(t.to[i]) + at, n, f);
-        else chunk_scale<F16>(static_cast<const _Float16 *>(t.from[i]) + at, static_cast<_Float16 *>(t.to[i]) + at, n, f);
+        const Chunk k = chunk_of(t, i, c);
+        if (t.type[i] == 0) chunk_scale<F32>(static_cast<const float *>(t.from[i]) + k.at, static_cast<float *>(t.to[i]) + k.at, k.n, f);
+        else if (t.type[i] == 1) chunk_scale<BF16>(static_cast<const __bf16 *>(t.from[i]) + k.at, static_cast<__bf16 *>(t.to[i]) + k.at, k.n, f);
+        else chunk_scale<F16>(static_cast<const _Float16 *>(t.from[i]) + k.at, static_cast<_Float16 *>(t.to[i]) + k.at, k.n, f);
     }
+}
+
+int64_t chunks_in(int64_t numel, int type)
+{
+    const int64_t items = kChunkBytes / type_bytes(type);
+    return (numel + items - 1) / items;
 }
 
 // The tensors from `i` on that go into one launch (empty ones left out); returns the first that does not.
@@ -164,16 +213,16 @@ int gather(Tensors &t, int i, const void *const *grads, void *const *outs, const
         t.to[t.n] = outs ? outs[i] : const_cast<void *>(t.from[t.n]);
         t.numel[t.n] = numels[i];
         t.type[t.n] = (uint8_t)types[i];
-        const int64_t end = t.first[t.n] + (numels[i] + kChunk - 1) / kChunk;
-        t.first[++t.n] = (int)end;                 // at most 2^40 / kChunk + kMostTensors chunks: below 2^31
+        const int64_t end = t.first[t.n] + chunks_in(numels[i], types[i]);
+        t.first[++t.n] = (int)end;                 // of 2^40 items at most: below 2^28
     }
     return i;
 }
 
-int64_t chunks_of(const int64_t *numels, int n)
+int64_t chunks_of(const int64_t *numels, const int32_t *types, int n)
 {
     int64_t c = 0;
-    for (int i = 0; i < n; ++i) c += (numels[i] + kChunk - 1) / kChunk;
+    for (int i = 0; i < n; ++i) c += chunks_in(numels[i], types[i]);
     return c;
 }
 
@@ -191,7 +240,7 @@ int blocks_of(const Tensors &t, int64_t all_chunks)
 int grad_parts(const int64_t *numels, const int32_t *types, int n)
 {
     Tensors t;
-    const int64_t all = chunks_of(numels, n);
+    const int64_t all = chunks_of(numels, types, n);
     int parts = 0;
     for (int i = 0; i < n;) {
         i = gather(t, i, nullptr, nullptr, numels, types, n);
@@ -204,7 +253,7 @@ hipError_t launch_grad_norm(const void *const *grads, const int64_t *numels, con
                             double *norm, hipStream_t s)
 {
     Tensors t;
-    const int64_t all = chunks_of(numels, n);
+    const int64_t all = chunks_of(numels, types, n);
     int at = 0;
     for (int i = 0; i < n;) {
         i = gather(t, i, grads, nullptr, numels, types, n);
@@ -221,7 +270,7 @@ hipError_t launch_grad_clip(const void *const *grads, void *const *outs, const i
                             double max_norm, double *norm, const double *parts, int n_parts, hipStream_t s)
 {
     Tensors t;
-    const int64_t all = chunks_of(numels, n);
+    const int64_t all = chunks_of(numels, types, n);
     int first = 1;
     for (int i = 0; i < n;) {
         i = gather(t, i, grads, outs, numels, types, n);
