@@ -364,8 +364,8 @@ int32_t cham_update_configs(uint8_t *theta, const int8_t *actions, int64_t B, in
 #define CHAM_TYPE_I32  17
 #define CHAM_TYPE_I64  18
 
-/* Bytes of DEVICE workspace of cham_policy_logp (want_grad = 0) and cham_policy_loss (0 without grad_logits, 1 with),
- * or a negative error. */
+/* Bytes of DEVICE workspace of cham_policy_logp (want_grad = 0) and cham_policy_loss (0 without grad_logits, 1 with:
+ * enough for either), or a negative error. */
 int64_t cham_policy_workspace_bytes(int64_t R, int32_t G, int32_t V, int32_t type, int32_t want_grad);
 
 /*

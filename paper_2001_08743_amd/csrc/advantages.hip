@@ -2,8 +2,9 @@
 //
 // A_t = b_t + c_t A_{t+1} with b_t = r_t + gamma n_t V_{t+1} - V_t and c_t = gamma lambda n_t is a composition of affine
 // maps: steps t .. u make of the advantage behind them q + p A_{u+1}, and two runs (p1, q1), (p2, q2), the second later, join
-// to (p1 p2, q1 + p1 q2).  So every thread folds a few consecutive steps, the runs of a workgroup are scanned from the end, and
-// every thread walks its steps once more with the advantage behind them known.
+// to (p1 p2, q1 + p1 q2).  So every thread folds eight consecutive steps, the runs of a workgroup's threads are scanned from the end,
+// and every thread walks its steps once more with the advantage behind them known: one read of everything, one write.  In
+// double: the sum over a long trajectory keeps its small terms, and the arithmetic is hidden behind memory all the same.
 #include "cham_device.h"
 #include "explore.h"
 #include "explore_items.h"
@@ -12,84 +13,13 @@ namespace cham {
 
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kSteps = 8;                 // consecutive steps of a thread
-constexpr int kTile = kThreads * kSteps;
 
 struct Run {
     double p, q;                          // factor and summand
 };
-__device__ __forceinline__ Run run_join(const Run &first, const Run &later) { return {first.p * later.p, first.q + first.p * later.q}; }
+__device__ __forceinline__ Run run_join(const Run &first, const Run &later) { return {first.p * later.p, __builtin_fma(first.p, later.q, first.q)}; }
 __device__ __forceinline__ Run run_down(const Run &r, int by) { return {__shfl_down(r.p, by), __shfl_down(r.q, by)}; }
-
-// Steps [t0, t1) of trajectory b from its end backwards, in tiles; `behind` is the advantage at t1.  WRITE: outputs; otherwise only
-// what the steps make of the advantage behind them, returned by thread 0.
-template <typename T, bool WRITE>
-__device__ Run walk(const GaeArgs &a, int64_t b, int64_t t0, int64_t t1, int64_t len, double behind)
-{
-    __shared__ Run waves[kThreads / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const typename T::item *rew = static_cast<const typename T::item *>(a.rewards) + b * a.r_ldb;
-    const typename T::item *val = static_cast<const typename T::item *>(a.values) + b * a.v_ldb;
-    const uint8_t *done = a.dones ? a.dones + b * a.d_ldb : nullptr;
-    const double boot = a.bootstrap ? (double)a.bootstrap[b] : 0.0;
-    const double gl = a.gamma * a.lambda;
-    Run all{1.0, 0.0};
-    for (int64_t hi = t1; hi > t0; hi -= kTile) {
-        const int64_t base = hi - kTile + (int64_t)tid * kSteps;       // may begin before t0
-        double c[kSteps], d[kSteps], v[kSteps];
-        double next = 0.0;
-        if (base + kSteps > t0) next = base + kSteps < len ? (double)T::get(val[(base + kSteps) * a.v_lds]) : boot;
-#pragma unroll
-        for (int i = kSteps - 1; i >= 0; --i) {
-            const int64_t t = base + i;
-            c[i] = 1.0;
-            d[i] = v[i] = 0.0;
-            if (t >= t0) {
-                const double n = done && done[t * a.d_lds] ? 0.0 : 1.0;
-                v[i] = (double)T::get(val[t * a.v_lds]);
-                d[i] = (double)T::get(rew[t * a.r_lds]) + a.gamma * n * next - v[i];
-                c[i] = gl * n;
-                next = v[i];
-            }
-        }
-        Run own{1.0, 0.0};
-#pragma unroll
-        for (int i = kSteps - 1; i >= 0; --i) own = run_join({c[i], d[i]}, own);
-        Run scan = own;                                                // this lane's steps and all behind them in the wave
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const Run r = run_down(scan, o);
-            if (lane + o < 64) scan = run_join(scan, r);
-        }
-        if (lane == 0) waves[wave] = scan;
-        Run later = run_down(scan, 1);
-        if (lane == 63) later = {1.0, 0.0};
-        __syncthreads();
-        Run rest{1.0, 0.0}, tile{1.0, 0.0};
-        for (int w = kThreads / 64 - 1; w >= 0; --w) {
-            if (w == wave) rest = tile;
-            tile = run_join(waves[w], tile);
-        }
-        if (WRITE) {
-            const Run r = run_join(later, rest);
-            double adv = r.q + r.p * behind;
-#pragma unroll
-            for (int i = kSteps - 1; i >= 0; --i) {
-                const int64_t t = base + i;
-                adv = d[i] + c[i] * adv;
-                if (t >= t0) {
-                    a.adv[b * a.o_ldb + t * a.o_lds] = (float)adv;
-                    if (a.ret) a.ret[b * a.o_ldb + t * a.o_lds] = (float)(adv + v[i]);
-                }
-            }
-            behind = tile.q + tile.p * behind;
-        }
-        all = run_join(tile, all);
-        __syncthreads();
-    }
-    return all;
-}
 
 __device__ __forceinline__ int64_t length_of(const GaeArgs &a, int64_t b)
 {
@@ -98,76 +28,301 @@ __device__ __forceinline__ int64_t length_of(const GaeArgs &a, int64_t b)
     return n < 0 ? 0 : n < a.S ? n : a.S;
 }
 
+// Eight steps of a thread: rewards, values, dones, and the value behind them.  Those outside [first, end) are none and do nothing; behind
+// step `boot_at` comes the bootstrap.
+struct Steps {
+    float r[kSteps], v[kSteps], next, boot;
+    uint32_t done;                        // a bit each
+    int first, end, boot_at;
+};
+
 template <typename T>
-__global__ void __launch_bounds__(kThreads) gae_kernel(const GaeArgs a)
+__device__ __forceinline__ void load_eight(const typename T::item *p, float (&x)[kSteps])
 {
-    for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
-        const int64_t len = length_of(a, b);
-        walk<T, true>(a, b, 0, len, len, 0.0);
+#pragma unroll
+    for (int k = 0; k < kSteps / T::kVec; ++k) {
+        const typename T::words w = *reinterpret_cast<const typename T::words *>(p + k * T::kVec);
+        float y[T::kVec];
+        T::unpack(make_uint4(w.x, w.y, w.z, w.w), y);
+#pragma unroll
+        for (int j = 0; j < T::kVec; ++j) x[k * T::kVec + j] = y[j];
     }
 }
 
-// Few long trajectories: chunks of one fold by themselves (gae_fold_kernel), then every chunk takes the advantage behind it from
-// the later ones' runs.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) gae_fold_kernel(const GaeArgs a)
+__device__ __forceinline__ int within(int64_t x) { return x < 0 ? 0 : x > kSteps ? kSteps : (int)x; }
+
+// Steps [base, base + 8) of trajectory b as far as they are in [lo, hi), hi at most its length.
+template <typename T, bool DENSE>
+__device__ __forceinline__ Steps load_steps(const GaeArgs &a, int64_t b, int64_t base, int64_t lo, int64_t hi, int64_t len)
 {
-    for (int64_t u = blockIdx.x; u < a.B * a.chunks; u += gridDim.x) {
-        const int64_t b = u / a.chunks, t0 = (u - b * a.chunks) * a.chunk, len = length_of(a, b);
-        const int64_t t1 = t0 + a.chunk < len ? t0 + a.chunk : len;
-        const Run r = walk<T, false>(a, b, t0, t1, len, 0.0);
-        if (threadIdx.x == 0) a.runs[u] = make_double2(r.p, r.q);
+    Steps s;
+    s.first = within(lo - base);
+    s.end = within(hi - base);
+    s.boot_at = len - 1 - base >= 0 && len - 1 - base < kSteps ? (int)(len - 1 - base) : -1;
+    s.done = 0;
+    s.next = s.boot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) s.r[i] = s.v[i] = 0.0f;
+    if (s.first >= s.end) return s;
+    const typename T::item *rew = static_cast<const typename T::item *>(a.rewards) + b * a.r_ldb + base * a.r_lds;
+    const typename T::item *val = static_cast<const typename T::item *>(a.values) + b * a.v_ldb + base * a.v_lds;
+    const uint8_t *done = a.dones ? a.dones + b * a.d_ldb + base * a.d_lds : nullptr;
+    if (base + kSteps < len) s.next = T::get(val[kSteps * a.v_lds]);
+    if (s.boot_at >= 0 && a.bootstrap) s.boot = a.bootstrap[b];
+    if (DENSE && s.first == 0 && s.end == kSteps) {
+        load_eight<T>(rew, s.r);
+        load_eight<T>(val, s.v);
+        if (done) {
+            typedef unsigned words __attribute__((ext_vector_type(2), aligned(1)));
+            const words w = *reinterpret_cast<const words *>(done);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) s.done |= (((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 0xffu) != 0 ? 1u << i : 0u;
+        }
+        return s;
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+        if (i >= s.first && i < s.end) {
+            s.r[i] = T::get(rew[i * a.r_lds]);
+            s.v[i] = T::get(val[i * a.v_lds]);
+            if (done && done[i * a.d_lds]) s.done |= 1u << i;
+        }
+    return s;
+}
+
+// What step i does to the advantage behind it.
+__device__ __forceinline__ Run step_of(const GaeArgs &a, const Steps &s, int i)
+{
+    const float next = i == s.boot_at ? s.boot : i == kSteps - 1 ? s.next : s.v[i + 1 < kSteps ? i + 1 : i];
+    const bool in = i >= s.first && i < s.end, done = (s.done >> i) & 1;
+    const double d = __builtin_fma(done ? 0.0 : a.gamma, (double)next, (double)s.r[i] - (double)s.v[i]);
+    return {in ? (done ? 0.0 : a.gamma_lambda) : 1.0, in ? d : 0.0};
+}
+__device__ __forceinline__ Run fold(const GaeArgs &a, const Steps &s)
+{
+    Run r = step_of(a, s, kSteps - 1);
+#pragma unroll
+    for (int i = kSteps - 2; i >= 0; --i) r = run_join(step_of(a, s, i), r);
+    return r;
+}
+template <bool DENSE>
+__device__ __forceinline__ void store_steps(const GaeArgs &a, int64_t b, const Steps &s, int64_t base, double behind)
+{
+    float adv[kSteps], ret[kSteps];
+#pragma unroll
+    for (int i = kSteps - 1; i >= 0; --i) {
+        const Run m = step_of(a, s, i);
+        behind = __builtin_fma(m.p, behind, m.q);
+        adv[i] = (float)behind;
+        ret[i] = (float)(behind + (double)s.v[i]);
+    }
+    const int64_t at = b * a.o_ldb + base * a.o_lds;
+    if (DENSE && s.first == 0 && s.end == kSteps) {
+        typedef float words __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+        for (int i = 0; i < kSteps; i += 4) {
+            *reinterpret_cast<words *>(a.adv + at + i) = words{adv[i], adv[i + 1], adv[i + 2], adv[i + 3]};
+            if (a.ret) *reinterpret_cast<words *>(a.ret + at + i) = words{ret[i], ret[i + 1], ret[i + 2], ret[i + 3]};
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+        if (i >= s.first && i < s.end) {
+            a.adv[at + i * a.o_lds] = adv[i];
+            if (a.ret) a.ret[at + i * a.o_lds] = ret[i];
+        }
+}
+
+// WIDTH trajectories side by side in a wave (1: a wave along time; lane = time group * WIDTH + trajectory).  A workgroup of THREADS walks steps [t0, t1) of its trajectories from the end
+// in tiles; `behind`: the advantage at t1.  WRITE: outputs; otherwise what the steps make of the advantage behind them is returned by
+// the threads of time group 0 of wave 0.
+template <typename T, int THREADS, int WIDTH, bool DENSE, bool WRITE>
+__device__ Run walk(const GaeArgs &a, int64_t b, int64_t t0, int64_t t1, int64_t last, double behind)
+{
+    constexpr int kWaves = THREADS / 64, kGroups = 64 / WIDTH, kTile = kWaves * kGroups * kSteps;
+    __shared__ Run waves[kWaves][WIDTH];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x % THREADS >> 6, group = lane / WIDTH, col = lane % WIDTH;
+    const bool there = b < a.B;
+    const int64_t len = there ? length_of(a, b) : 0;
+    const int64_t hi_all = t1 < last ? t1 : last;          // the longest of the trajectories side by side
+    const int64_t end = t1 < len ? t1 : len;
+    Run all{1.0, 0.0};
+    for (int64_t hi = hi_all; hi > t0; hi -= kTile) {
+        const int64_t base = hi - kTile + (int64_t)(wave * kGroups + group) * kSteps;       // may begin before t0
+        const int64_t top = hi < end ? hi : end;
+        const Steps s = load_steps<T, DENSE>(a, there ? b : 0, base, t0, there ? top : t0, len);
+        Run scan = fold(a, s);                                // this thread's steps and all behind them in the wave
+#pragma unroll
+        for (int o = WIDTH; o < 64; o <<= 1) {
+            const Run r = run_down(scan, o);
+            if (lane + o < 64) scan = run_join(scan, r);
+        }
+        Run later = run_down(scan, WIDTH & 63);
+        if (group == kGroups - 1) later = {1.0, 0.0};
+        Run tile = scan, rest{1.0, 0.0};
+        if (kWaves > 1) {
+            if (group == 0) waves[wave][col] = scan;
+            __syncthreads();
+            tile = {1.0, 0.0};
+#pragma unroll 2
+            for (int w = kWaves - 1; w >= 0; --w) {
+                if (w == wave) rest = tile;
+                tile = run_join(waves[w][col], tile);
+            }
+            __syncthreads();
+        } else {
+            tile = {__shfl(scan.p, col), __shfl(scan.q, col)};
+        }
+        if (WRITE) {
+            const Run r = run_join(later, rest);
+            if (there) store_steps<DENSE>(a, b, s, base, __builtin_fma(r.p, behind, r.q));
+            behind = __builtin_fma(tile.p, behind, tile.q);
+        }
+        all = run_join(tile, all);
+    }
+    return all;
+}
+
+// The advantage behind chunk i of a trajectory, from the runs of the later ones: a lane joins some consecutive ones, then the lanes.
+__device__ __forceinline__ double behind_chunk(const GaeArgs &a, int64_t b, int i)
+{
+    const int lane = threadIdx.x & 63, n = a.chunks - 1 - i, per = (n + 63) / 64;
+    Run r{1.0, 0.0};
+    for (int k = per - 1; k >= 0; --k) {
+        const int j = i + 1 + lane * per + k;
+        if (j < a.chunks && b < a.B) {
+            const double2 x = a.runs[b * a.chunks + j];
+            r = run_join({x.x, x.y}, r);
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const Run x = run_down(r, o);
+        if (lane + o < 64) r = run_join(r, x);
+    }
+    return __shfl(r.q, 0);
+}
+
+// MODE 0: whole trajectories.  Few long ones are cut into chunks: 1 folds each by itself, 2 takes the advantage behind a chunk from the runs of
+// the later ones and writes.
+template <typename T, int THREADS, bool DENSE, int MODE>
+__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) gae_row_kernel(const GaeArgs a)
+{
+    constexpr int kRows = THREADS < 256 ? 256 / THREADS : 1;
+    static_assert(THREADS == 64 || kRows == 1, "a wave needs no barrier with its neighbours");
+    const int row = kRows > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
+    const int64_t units = a.B * a.chunks;
+    for (int64_t u = (int64_t)blockIdx.x * kRows + row; u < units; u += (int64_t)gridDim.x * kRows) {
+        const int64_t b = u / a.chunks;
+        const int i = (int)(u - b * a.chunks);
+        const int64_t t0 = i * a.chunk, t1 = MODE == 0 ? a.S : t0 + a.chunk, last = length_of(a, b);
+        if (MODE == 1) {
+            const Run r = walk<T, THREADS, 1, DENSE, false>(a, b, t0, t1, last, 0.0);
+            if (threadIdx.x % THREADS == 0) a.runs[u] = make_double2(r.p, r.q);
+        } else {
+            walk<T, THREADS, 1, DENSE, true>(a, b, t0, t1, last, MODE == 2 ? behind_chunk(a, b, i) : 0.0);
+        }
     }
 }
-template <typename T>
-__global__ void __launch_bounds__(kThreads) gae_chunk_kernel(const GaeArgs a)
+
+// Trajectories side by side in memory, steps one after the other: sixteen trajectories a workgroup, 64 bytes of each step.
+constexpr int kWidth = 16, kSideThreads = 1024;
+template <typename T, int MODE>
+__global__ void __launch_bounds__(kSideThreads) gae_side_kernel(const GaeArgs a)
 {
-    for (int64_t u = blockIdx.x; u < a.B * a.chunks; u += gridDim.x) {
-        const int64_t b = u / a.chunks, i = u - b * a.chunks, t0 = i * a.chunk, len = length_of(a, b);
-        const int64_t t1 = t0 + a.chunk < len ? t0 + a.chunk : len;
-        double behind = 0.0;
-        for (int64_t j = a.chunks - 1; j > i; --j) {
-            const double2 r = a.runs[b * a.chunks + j];
-            behind = r.y + r.x * behind;
+    const int64_t sets = (a.B + kWidth - 1) / kWidth, units = sets * a.chunks;
+    const int col = threadIdx.x % kWidth;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int64_t set = u / a.chunks, b = set * kWidth + col;
+        const int i = (int)(u - set * a.chunks);
+        int64_t last = b < a.B ? length_of(a, b) : 0;
+#pragma unroll
+        for (int o = 1; o < kWidth; o <<= 1) {
+            const int64_t x = __shfl_xor(last, o);
+            last = x > last ? x : last;
         }
-        walk<T, true>(a, b, t0, t1, len, behind);
+        const int64_t t0 = i * a.chunk, t1 = MODE == 0 ? a.S : t0 + a.chunk;
+        if (MODE == 1) {
+            const Run r = walk<T, kSideThreads, kWidth, false, false>(a, b, t0, t1, last, 0.0);
+            if (threadIdx.x < kWidth && b < a.B) a.runs[b * a.chunks + i] = make_double2(r.p, r.q);
+        } else {
+            double behind = 0.0;
+            if (MODE == 2 && b < a.B)
+                for (int j = a.chunks - 1; j > i; --j) {
+                    const double2 x = a.runs[b * a.chunks + j];
+                    behind = __builtin_fma(x.x, behind, x.y);
+                }
+            walk<T, kSideThreads, kWidth, false, true>(a, b, t0, t1, last, behind);
+        }
     }
+}
+
+constexpr int64_t kMostBlocks = 1 << 20;
+unsigned blocks_for(int64_t n) { return (unsigned)(n < kMostBlocks ? n : kMostBlocks); }
+
+template <typename T, int THREADS, bool DENSE>
+void launch_row(const GaeArgs &a, hipStream_t s)
+{
+    constexpr int kBlock = THREADS < 256 ? 256 : THREADS, kRows = kBlock / THREADS;
+    const dim3 grid(blocks_for((a.B * a.chunks + kRows - 1) / kRows));
+    if (a.chunks == 1) {
+        hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, 0>), grid, dim3(kBlock), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, 1>), grid, dim3(kBlock), 0, s, a);
+        hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, 2>), grid, dim3(kBlock), 0, s, a);
+    }
+}
+template <typename T, int THREADS>
+void launch_row_of(const GaeArgs &a, hipStream_t s)
+{
+    const bool dense = a.r_lds == 1 && a.v_lds == 1 && (!a.dones || a.d_lds == 1) && a.o_lds == 1;
+    if (dense) launch_row<T, THREADS, true>(a, s);
+    else launch_row<T, THREADS, false>(a, s);
 }
 
 template <typename T>
 hipError_t launch_typed(const GaeArgs &a, hipStream_t s)
 {
-    const int64_t units = a.B * a.chunks;
-    const dim3 grid((unsigned)(units < (1 << 20) ? units : (1 << 20)));
-    if (a.chunks == 1) {
-        hipLaunchKernelGGL(gae_kernel<T>, grid, dim3(kThreads), 0, s, a);
+    if (a.side) {
+        const dim3 grid(blocks_for((a.B + kWidth - 1) / kWidth * a.chunks));
+        if (a.chunks == 1) {
+            hipLaunchKernelGGL((gae_side_kernel<T, 0>), grid, dim3(kSideThreads), 0, s, a);
+        } else {
+            hipLaunchKernelGGL((gae_side_kernel<T, 1>), grid, dim3(kSideThreads), 0, s, a);
+            hipLaunchKernelGGL((gae_side_kernel<T, 2>), grid, dim3(kSideThreads), 0, s, a);
+        }
+    } else if (a.threads == 64) {
+        launch_row_of<T, 64>(a, s);
+    } else if (a.threads == 256) {
+        launch_row_of<T, 256>(a, s);
     } else {
-        hipLaunchKernelGGL(gae_fold_kernel<T>, grid, dim3(kThreads), 0, s, a);
-        hipLaunchKernelGGL(gae_chunk_kernel<T>, grid, dim3(kThreads), 0, s, a);
+        launch_row_of<T, 1024>(a, s);
     }
     return hipGetLastError();
 }
 
 }  // namespace
 
-GaePlan plan_gae(int64_t B, int64_t S)
+GaePlan plan_gae(int64_t B, int64_t S, bool side)
 {
-    // chunks of whole tiles, until there are 512 workgroups
-    const int64_t tiles = (S + kTile - 1) / kTile;
-    const int64_t want = B > 0 ? (512 + B - 1) / B : 1;
+    GaePlan p;
+    // chunks of whole tiles, until there are two workgroups for every compute unit
+    p.threads = side ? kSideThreads : S <= 512 ? 64 : S <= 2048 ? 256 : 1024;
+    const int64_t tile = side ? kSideThreads / kWidth * kSteps : (int64_t)p.threads * kSteps;
+    const int64_t tiles = (S + tile - 1) / tile, units = side ? (B + kWidth - 1) / kWidth : B;
+    const int64_t want = units > 0 ? (512 + units - 1) / units : 1;
     int64_t n = want < tiles ? want : tiles;
     if (n < 1) n = 1;
-    const int64_t per = (tiles + n - 1) / n;
-    GaePlan p;
-    p.chunk = (per > 0 ? per : 1) * kTile;
+    const int64_t per = tiles > 0 ? (tiles + n - 1) / n : 1;
+    p.chunk = per * tile;
     p.chunks = tiles > 0 ? (int)((tiles + per - 1) / per) : 1;
     p.bytes = p.chunks > 1 ? (B * p.chunks * 16 + 255) / 256 * 256 : 0;
     return p;
 }
 
-hipError_t launch_gae(GaeArgs a, int type, hipStream_t s)
+hipError_t launch_gae(const GaeArgs &a, int type, hipStream_t s)
 {
-    if (a.B == 0 || a.S == 0) return hipSuccess;
     return type == 0 ? launch_typed<F32>(a, s) : type == 1 ? launch_typed<BF16>(a, s) : launch_typed<F16>(a, s);
 }
 

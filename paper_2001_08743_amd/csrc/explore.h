@@ -52,18 +52,21 @@ struct GaeArgs {
     int64_t r_ldb, r_lds, v_ldb, v_lds, d_ldb, d_lds, o_ldb, o_lds;
     const float *bootstrap;
     const int *lengths;
-    double gamma, lambda;
+    double gamma, gamma_lambda;
     float *adv, *ret;
     double2 *runs;                 // [B][chunks] what a chunk makes of the advantage behind it: factor, summand
     int64_t chunk;                 // steps of a chunk (S rounded up: one chunk)
     int chunks;
+    int threads;                   // of a trajectory
+    bool side;                     // steps of trajectories side by side
 };
+// side: the steps of neighbouring trajectories are neighbours in memory.
 struct GaePlan {
-    int chunks;
+    int threads, chunks;
     int64_t chunk, bytes;
 };
-GaePlan plan_gae(int64_t B, int64_t S);
-hipError_t launch_gae(GaeArgs a, int type, hipStream_t s);
+GaePlan plan_gae(int64_t B, int64_t S, bool side);
+hipError_t launch_gae(const GaeArgs &a, int type, hipStream_t s);
 
 int grad_parts(const int64_t *numels, const int32_t *types, int n);     // partial sums a norm needs room for
 hipError_t launch_grad_norm(const void *const *grads, const int64_t *numels, const int32_t *types, int n, double *parts, int n_parts,

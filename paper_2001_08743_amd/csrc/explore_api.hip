@@ -78,7 +78,9 @@ int64_t cham_policy_workspace_bytes(int64_t R, int32_t G, int32_t V, int32_t typ
 {
     const int32_t e = check_sizes(R, G, V, type);
     if (e != CHAM_OK) return e;
-    return plan_policy(R, G, V, type, want_grad != 0).bytes;
+    // with gradients: enough for either call
+    const int64_t without = plan_policy(R, G, V, type, false).bytes, with = want_grad ? plan_policy(R, G, V, type, true).bytes : 0;
+    return with > without ? with : without;
 }
 
 int32_t cham_policy_logp(const void *logits, int32_t type, int64_t R, int32_t G, int32_t V, int64_t ld_r, int64_t ld_g,
@@ -152,7 +154,9 @@ int32_t cham_policy_loss(const void *logits, int32_t type, int64_t R, int32_t G,
 int64_t cham_gae_workspace_bytes(int64_t B, int64_t S)
 {
     if (B < 0 || S < 0 || S > 0x7fffffff || (S > 0 && B > kMostItems / S)) return CHAM_E_BAD_DIM;
-    return plan_gae(B, S).bytes;
+    // the larger one: the query does not ask for the layout
+    const int64_t row = plan_gae(B, S, false).bytes, side = plan_gae(B, S, true).bytes;
+    return row > side ? row : side;
 }
 
 int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_t r_ldb, int64_t r_lds,
@@ -182,7 +186,9 @@ int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_
         !aligned(advantages, 4) || !aligned(returns, 4))
         return CHAM_E_BAD_DIM;
     if (!workspace_ok(workspace, workspace_bytes, need)) return CHAM_E_WORKSPACE;
-    const GaePlan p = plan_gae(B, S);
+    // trajectories side by side: rewards, values and outputs of a step stand closer together than the steps of a trajectory
+    const bool side = B >= 8 && r_ldb < r_lds && v_ldb < v_lds && o_ldb < o_lds;
+    const GaePlan p = plan_gae(B, S, side);
     GaeArgs a{};
     a.B = B;
     a.S = S;
@@ -200,12 +206,14 @@ int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_
     a.bootstrap = bootstrap;
     a.lengths = lengths;
     a.gamma = gamma;
-    a.lambda = lambda;
+    a.gamma_lambda = gamma * lambda;
     a.adv = advantages;
     a.ret = returns;
     a.runs = static_cast<double2 *>(workspace);
     a.chunk = p.chunk;
     a.chunks = p.chunks;
+    a.threads = p.threads;
+    a.side = side;
     const hipError_t h = launch_gae(a, type, reinterpret_cast<hipStream_t>(stream));
     return h == hipSuccess ? CHAM_OK : hip_fail(h);
 }
