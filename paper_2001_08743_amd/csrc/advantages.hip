@@ -138,21 +138,20 @@ __device__ __forceinline__ void store_steps(const GaeArgs &a, int64_t b, const S
 // in tiles; `behind`: the advantage at t1.  WRITE: outputs; otherwise what the steps make of the advantage behind them is returned by
 // the threads of time group 0 of wave 0.
 template <typename T, int THREADS, int WIDTH, bool DENSE, bool WRITE>
-__device__ Run walk(const GaeArgs &a, int64_t b, int64_t t0, int64_t t1, int64_t last, double behind)
+__device__ Run walk(const GaeArgs &a, int64_t b, int64_t t0, int64_t t1, int64_t len, int64_t last, double behind)
 {
     constexpr int kWaves = THREADS / 64, kGroups = 64 / WIDTH, kTile = kWaves * kGroups * kSteps;
     __shared__ Run waves[kWaves][WIDTH];
     const int lane = threadIdx.x & 63, wave = threadIdx.x % THREADS >> 6, group = lane / WIDTH, col = lane % WIDTH;
-    const bool there = b < a.B;
-    const int64_t len = there ? length_of(a, b) : 0;
     const int64_t hi_all = t1 < last ? t1 : last;          // the longest of the trajectories side by side
     const int64_t end = t1 < len ? t1 : len;
     Run all{1.0, 0.0};
     for (int64_t hi = hi_all; hi > t0; hi -= kTile) {
         const int64_t base = hi - kTile + (int64_t)(wave * kGroups + group) * kSteps;       // may begin before t0
         const int64_t top = hi < end ? hi : end;
-        const Steps s = load_steps<T, DENSE>(a, there ? b : 0, base, t0, there ? top : t0, len);
-        Run scan = fold(a, s);                                // this thread's steps and all behind them in the wave
+        const Steps s = load_steps<T, DENSE>(a, b, base, t0, top, len);
+        Run scan{1.0, 0.0};
+        if (__any(s.first < s.end)) scan = fold(a, s);                                // this thread's steps and all behind them in the wave
 #pragma unroll
         for (int o = WIDTH; o < 64; o <<= 1) {
             const Run r = run_down(scan, o);
@@ -176,7 +175,7 @@ __device__ Run walk(const GaeArgs &a, int64_t b, int64_t t0, int64_t t1, int64_t
         }
         if (WRITE) {
             const Run r = run_join(later, rest);
-            if (there) store_steps<DENSE>(a, b, s, base, __builtin_fma(r.p, behind, r.q));
+            if (s.first < s.end) store_steps<DENSE>(a, b, s, base, __builtin_fma(r.p, behind, r.q));
             behind = __builtin_fma(tile.p, behind, tile.q);
         }
         all = run_join(tile, all);
@@ -207,21 +206,21 @@ __device__ __forceinline__ double behind_chunk(const GaeArgs &a, int64_t b, int 
 // MODE 0: whole trajectories.  Few long ones are cut into chunks: 1 folds each by itself, 2 takes the advantage behind a chunk from the runs of
 // the later ones and writes.
 template <typename T, int THREADS, bool DENSE, int MODE>
-__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) gae_row_kernel(const GaeArgs a)
+__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS > 64 ? 4 : 2) gae_row_kernel(const GaeArgs a)
 {
     constexpr int kRows = THREADS < 256 ? 256 / THREADS : 1;
     static_assert(THREADS == 64 || kRows == 1, "a wave needs no barrier with its neighbours");
     const int row = kRows > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
     const int64_t units = a.B * a.chunks;
     for (int64_t u = (int64_t)blockIdx.x * kRows + row; u < units; u += (int64_t)gridDim.x * kRows) {
-        const int64_t b = u / a.chunks;
-        const int i = (int)(u - b * a.chunks);
-        const int64_t t0 = i * a.chunk, t1 = MODE == 0 ? a.S : t0 + a.chunk, last = length_of(a, b);
+        const int64_t b = MODE == 0 ? u : u / a.chunks;
+        const int i = MODE == 0 ? 0 : (int)(u - b * a.chunks);
+        const int64_t t0 = i * a.chunk, t1 = MODE == 0 ? a.S : t0 + a.chunk, len = length_of(a, b);
         if (MODE == 1) {
-            const Run r = walk<T, THREADS, 1, DENSE, false>(a, b, t0, t1, last, 0.0);
+            const Run r = walk<T, THREADS, 1, DENSE, false>(a, b, t0, t1, len, len, 0.0);
             if (threadIdx.x % THREADS == 0) a.runs[u] = make_double2(r.p, r.q);
         } else {
-            walk<T, THREADS, 1, DENSE, true>(a, b, t0, t1, last, MODE == 2 ? behind_chunk(a, b, i) : 0.0);
+            walk<T, THREADS, 1, DENSE, true>(a, b, t0, t1, len, len, MODE == 2 ? behind_chunk(a, b, i) : 0.0);
         }
     }
 }
@@ -234,9 +233,10 @@ __global__ void __launch_bounds__(kSideThreads) gae_side_kernel(const GaeArgs a)
     const int64_t sets = (a.B + kWidth - 1) / kWidth, units = sets * a.chunks;
     const int col = threadIdx.x % kWidth;
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int64_t set = u / a.chunks, b = set * kWidth + col;
+        const int64_t set = MODE == 0 ? u : u / a.chunks, b = set * kWidth + col;
         const int i = (int)(u - set * a.chunks);
-        int64_t last = b < a.B ? length_of(a, b) : 0;
+        const int64_t len = b < a.B ? length_of(a, b) : 0;              // 0: nothing of it is read or written
+        int64_t last = len;                                             // the longest of those side by side
 #pragma unroll
         for (int o = 1; o < kWidth; o <<= 1) {
             const int64_t x = __shfl_xor(last, o);
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kSideThreads) gae_side_kernel(const GaeArgs a)
         }
         const int64_t t0 = i * a.chunk, t1 = MODE == 0 ? a.S : t0 + a.chunk;
         if (MODE == 1) {
-            const Run r = walk<T, kSideThreads, kWidth, false, false>(a, b, t0, t1, last, 0.0);
+            const Run r = walk<T, kSideThreads, kWidth, false, false>(a, b, t0, t1, len, last, 0.0);
             if (threadIdx.x < kWidth && b < a.B) a.runs[b * a.chunks + i] = make_double2(r.p, r.q);
         } else {
             double behind = 0.0;
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kSideThreads) gae_side_kernel(const GaeArgs a)
                     const double2 x = a.runs[b * a.chunks + j];
                     behind = __builtin_fma(x.x, behind, x.y);
                 }
-            walk<T, kSideThreads, kWidth, false, true>(a, b, t0, t1, last, behind);
+            walk<T, kSideThreads, kWidth, false, true>(a, b, t0, t1, len, last, behind);
         }
     }
 }
@@ -297,7 +297,7 @@ hipError_t launch_typed(const GaeArgs &a, hipStream_t s)
     } else if (a.threads == 256) {
         launch_row_of<T, 256>(a, s);
     } else {
-        launch_row_of<T, 1024>(a, s);
+        launch_row_of<T, 512>(a, s);
     }
     return hipGetLastError();
 }
@@ -308,7 +308,7 @@ GaePlan plan_gae(int64_t B, int64_t S, bool side)
 {
     GaePlan p;
     // chunks of whole tiles, until there are two workgroups for every compute unit
-    p.threads = side ? kSideThreads : S <= 512 ? 64 : S <= 2048 ? 256 : 1024;
+    p.threads = side ? kSideThreads : S <= 512 ? 64 : S <= 2048 || B * ((S + 4095) / 4096) < 256 ? 256 : 512;
     const int64_t tile = side ? kSideThreads / kWidth * kSteps : (int64_t)p.threads * kSteps;
     const int64_t tiles = (S + tile - 1) / tile, units = side ? (B + kWidth - 1) / kWidth : B;
     const int64_t want = units > 0 ? (512 + units - 1) / units : 1;
