@@ -36,6 +36,7 @@ struct PolicyArgs {
 
 // How a call is run; a function of its sizes and type alone, so that the workspace can be asked for ahead of it.
 struct PolicyPlan {
+    int lanes;                     // up to four choices a head: lanes of a decision; 0 elsewhere
     int tile;                      // few choices a head: decisions of a tile; 0 elsewhere
     int row, threads;              // one head: 16-byte pieces of a row that each of so many threads holds; 0 elsewhere
     int splits;                    // workgroups a head is split over

@@ -84,7 +84,7 @@ __device__ __forceinline__ Soft soft_join(Soft a, Soft b)
 __device__ __forceinline__ float2 log_and_entropy(const Soft &v)
 {
     const float ls = logf(v.s);
-    return make_float2(ls, ls - v.t * kLn2 / v.s);
+    return make_float2(ls, ls - v.t * kLn2 * __builtin_amdgcn_rcpf(v.s));
 }
 
 // Gradient by a head's logits: 2^z (c0 + c1 z), and D more at the action.
@@ -94,7 +94,7 @@ struct Slope {
 };
 __device__ __forceinline__ Slope slope_of(float m, float s, float ls, float entropy, float2 d)
 {
-    const float inv = 1.0f / s;
+    const float inv = __builtin_amdgcn_rcpf(s);              // within an ulp; s is at least e^-8 and at most e^8 V
     return {scale_of(m), (d.y * (entropy - ls) - d.x) * inv, d.y * kLn2 * inv};
 }
 template <bool ENT>
@@ -310,7 +310,7 @@ constexpr int kTileChoices = 32;                // beyond, a tile has fewer head
 struct TileShape {
     int per_tile;           // decisions of a tile
     int stride;             // of a head's logits in LDS: odd, so that the threads of a wave read different banks
-    unsigned inv_v, inv_gv; // ceil(2^32 / V), ceil(2^32 / (G V)): quotients of item numbers below 2^16
+    unsigned inv_v, inv_g;  // ceil(2^32 / V), ceil(2^32 / G): quotients of numbers below 2^16
     int dense;              // the logits of a tile are one run of items
     int gdense;             // its gradients are
 };
@@ -347,13 +347,164 @@ __device__ __forceinline__ void write_run(typename T::item *p, int n, F &&f)
     }
 }
 
+// Sums of a tile's decisions over their heads, in LDS, and what follows from them: dec, and in[] of the heads whose decision does not count.
+// given: of decision tid, asked for ahead of the heads.
+template <int HEADS>
+struct TileHeads {
+    float2 one[HEADS];          // log-probability and entropy of a head
+    float2 dec[HEADS];          // of a decision: (D, w c_H)
+    uint8_t in[HEADS];
+};
+template <int HEADS>
+__device__ __forceinline__ void decide_tile(const PolicyArgs &a, TileHeads<HEADS> &t, int64_t r0, int nr, const Given &given, double *sum)
+{
+    for (int r = threadIdx.x; r < nr; r += kThreads) {
+        double lp = 0.0, H = 0.0;
+        bool any = false;
+        if (counts(a, r0 + r))
+#pragma unroll 4
+            for (int g = 0; g < a.G; ++g) {
+                const float2 o = t.one[r * a.G + g];
+                lp += (double)o.x;
+                H += (double)o.y;
+                any = any || t.in[r * a.G + g] != 0;
+            }
+        t.dec[r] = decide(a, r0 + r, r < kThreads ? given : given_of(a, r0 + r, load_plain), any, lp, H, sum);
+        if (!any)                           // also of weight 0: zeros, whatever the logits are
+            for (int g = 0; g < a.G; ++g) t.in[r * a.G + g] = 0;
+    }
+}
+
+// A head's log-probability from its sums; c = -1: left out.
+__device__ __forceinline__ float2 head_of(const PolicyArgs &a, Soft &v, float xa, int &c, float2 &le)
+{
+    if (c < 0) return make_float2(0.0f, 0.0f);
+    if (c == a.V) {
+        c = 0;
+        le.x = le.y = v.s = __builtin_nanf("");
+        return le;
+    }
+    if (v.s == 0.0f) {
+        c = -1;                                 // every choice is masked
+        return make_float2(0.0f, 0.0f);
+    }
+    le = log_and_entropy(v);
+    return make_float2(xa - v.m - le.x, le.y);
+}
+
+// Up to four choices: a lane holds HEADS consecutive heads of a decision, as many lanes as it takes side by side a decision, and a wave as
+// many decisions as fit (24 heads: six lanes, ten decisions).  Nothing goes through LDS and no wave waits for another.
+template <typename T, int V, int HEADS>
+__global__ void __launch_bounds__(kThreads, 4) policy_lane_kernel(const PolicyArgs a, int lanes)
+{
+    const int lane = threadIdx.x & 63, per_wave = 64 / lanes, mine = lane / lanes, part = lane - mine * lanes;
+    const int64_t step = (int64_t)gridDim.x * (kThreads / 64) * per_wave;
+    const int h0 = part * HEADS, n = mine < per_wave ? (a.G - h0 < HEADS ? a.G - h0 : HEADS) : 0;      // heads of this lane
+    const bool dense = (a.G == 1 || a.ld_g == V) && n == HEADS, gdense = (a.G == 1 || a.gld_g == V) && n == HEADS;
+    double sum[kPolicySums] = {};
+    for (int64_t r0 = ((int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * per_wave; r0 < a.R; r0 += step) {
+        const int64_t r = r0 + mine;
+        const int here = r < a.R ? n : 0;
+        float x[HEADS][V];
+        int c[HEADS];
+        Given given{};
+        bool on = false;
+#pragma unroll
+        for (int u = 0; u < HEADS; ++u) {
+            c[u] = -1;
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[u][j] = 0.0f;
+        }
+        if (here > 0) {
+            const typename T::item *p = static_cast<const typename T::item *>(a.logits) + r * a.ld_r + h0 * a.ld_g;
+            if (dense) {
+                typename T::item y[HEADS * V];
+#pragma unroll
+                for (int i = 0; i < HEADS * V; ++i) y[i] = p[i];
+#pragma unroll
+                for (int i = 0; i < HEADS * V; ++i) x[i / V][i % V] = T::get(y[i]);
+            } else {
+#pragma unroll
+                for (int u = 0; u < HEADS; ++u)
+                    if (u < here)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) x[u][j] = T::get(p[u * a.ld_g + j]);
+            }
+#pragma unroll
+            for (int u = 0; u < HEADS; ++u)
+                if (u < here) c[u] = choice_of(a, r * a.G + h0 + u);
+            if (part == 0) given = given_of(a, r, load_plain);
+            on = counts(a, r);
+        }
+        Soft v[HEADS];
+        float2 le[HEADS];
+        double lp = 0.0, H = 0.0;
+        bool any = false;
+#pragma unroll
+        for (int u = 0; u < HEADS; ++u) {
+            v[u] = soft_none();
+            le[u] = make_float2(0.0f, 0.0f);
+            float xa = 0.0f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                v[u].m = fmaxf(v[u].m, x[u][j]);
+                xa = j == c[u] ? x[u][j] : xa;
+            }
+            const Scale k2 = scale_of(v[u].m);
+#pragma unroll
+            for (int j = 0; j < V; ++j) soft_add(v[u], x[u][j], k2);
+            const float2 one = head_of(a, v[u], xa, c[u], le[u]);
+            lp += (double)one.x;
+            H += (double)one.y;
+            any = any || c[u] >= 0;
+        }
+        // the decision's lanes joined into its first one
+        for (int o = 1; o < lanes; o <<= 1) {
+            const double l2 = __shfl_down(lp, o), H2 = __shfl_down(H, o);
+            const int a2 = __shfl_down((int)any, o);
+            if (part + o < lanes) {
+                lp += l2;
+                H += H2;
+                any = any || a2;
+            }
+        }
+        float2 d = make_float2(0.0f, 0.0f);
+        on = on && any;
+        if (part == 0 && here > 0) d = decide(a, r, given, on, on ? lp : 0.0, on ? H : 0.0, sum);
+        if (!a.grad) continue;
+        const int first = lane - part;
+        d = make_float2(__shfl(d.x, first), __shfl(d.y, first));
+        on = __shfl((int)on, first);
+        if (here == 0) continue;
+        typename T::item *p = static_cast<typename T::item *>(a.grad) + r * a.gld_r + h0 * a.gld_g;
+        typename T::item y[HEADS * V];
+#pragma unroll
+        for (int u = 0; u < HEADS; ++u) {
+            const bool in = on && c[u] >= 0;
+            const Slope f = slope_of(v[u].m, v[u].s, le[u].x, le[u].y, d);
+#pragma unroll
+            for (int j = 0; j < V; ++j) y[u * V + j] = T::put(in ? slope_at<true>(f, x[u][j]) + (j == c[u] ? d.x : 0.0f) : 0.0f);
+        }
+        if (gdense) {
+#pragma unroll
+            for (int i = 0; i < HEADS * V; ++i) p[i] = y[i];
+        } else {
+#pragma unroll
+            for (int u = 0; u < HEADS; ++u)
+                if (u < here)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) p[u * a.gld_g + j] = y[u * V + j];
+        }
+    }
+    if (a.old_logp) store_sums<kThreads / 64>(a, sum);
+}
+
+// More: the tile's logits in LDS, eight at a time in a thread's registers.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs a, const TileShape k)
 {
     __shared__ float x[kTileItems];
-    __shared__ float2 one[kTileHeads];          // log-probability and entropy of a head
-    __shared__ float2 dec[kTileHeads];          // of a decision: (D, w c_H)
-    __shared__ uint8_t in[kTileHeads];
+    __shared__ TileHeads<kTileHeads> t;
     const int tid = threadIdx.x;
     const int gv = a.G * a.V;
     double sum[kPolicySums] = {};
@@ -365,9 +516,17 @@ __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs 
             return i + h;
         };
         auto offset = [&](int i, int64_t ld_r, int64_t ld_g) {
-            const int h = quotient(i, k.inv_v, a.V), r = quotient(i, k.inv_gv, gv);
+            const int h = quotient(i, k.inv_v, a.V), r = quotient(h, k.inv_g, a.G);
             return (r0 + r) * ld_r + (h - r * a.G) * ld_g + (i - h * a.V);
         };
+        int c[kHeadsPerThread];
+#pragma unroll
+        for (int u = 0; u < kHeadsPerThread; ++u) {
+            const int h = tid + u * kThreads;
+            c[u] = h < heads ? choice_of(a, r0 * a.G + h) : -1;
+        }
+        Given given{};
+        if (tid < nr) given = given_of(a, r0 + tid, load_plain);
         const typename T::item *logits = static_cast<const typename T::item *>(a.logits);
         if (k.dense)
             read_run<T>(logits + r0 * gv, items, [&](int i, float v) { x[at(i)] = v; });
@@ -377,67 +536,39 @@ __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs 
 
         Soft v[kHeadsPerThread];
         float2 le[kHeadsPerThread];
-        int c[kHeadsPerThread];
 #pragma unroll
         for (int u = 0; u < kHeadsPerThread; ++u) {
             const int h = tid + u * kThreads;
             v[u] = soft_none();
             le[u] = make_float2(0.0f, 0.0f);
-            c[u] = -1;
             if (h >= heads) continue;
             const float *xh = x + h * k.stride;
-            c[u] = choice_of(a, r0 * a.G + h);
-            float lp = 0.0f;
-            if (c[u] == a.V) {
-                c[u] = 0;
-                le[u].x = le[u].y = v[u].s = lp = __builtin_nanf("");
-            } else if (c[u] >= 0) {
-                for (int j = 0; j < a.V; ++j) v[u].m = fmaxf(v[u].m, xh[j]);
-                const Scale k2 = scale_of(v[u].m);
-                for (int j = 0; j < a.V; ++j) soft_add(v[u], xh[j], k2);
-                if (v[u].s != 0.0f) {
-                    le[u] = log_and_entropy(v[u]);
-                    lp = xh[c[u]] - v[u].m - le[u].x;
-                } else {
-                    c[u] = -1;                  // every choice is masked
-                }
+            Scale k2 = scale_of(v[u].m);
+            for (int j0 = 0; j0 < a.V; j0 += 8) {
+                float y[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = j0 + j < a.V ? xh[j0 + j] : -__builtin_inff();
+                soft_add_all(v[u], k2, y);
             }
-            one[h] = make_float2(lp, le[u].y);
-            in[h] = c[u] >= 0;
+            const float xa = c[u] >= 0 && c[u] < a.V ? xh[c[u]] : 0.0f;
+            t.one[h] = head_of(a, v[u], xa, c[u], le[u]);
+            t.in[h] = c[u] >= 0;
         }
         __syncthreads();
-        for (int r = tid; r < nr; r += kThreads) {
-            double lp = 0.0, H = 0.0;
-            bool any = false;
-            if (counts(a, r0 + r))
-                for (int g = 0; g < a.G; ++g) {
-                    const float2 o = one[r * a.G + g];
-                    lp += (double)o.x;
-                    H += (double)o.y;
-                    any = any || in[r * a.G + g] != 0;
-                }
-            dec[r] = decide(a, r0 + r, given_of(a, r0 + r, load_plain), any, lp, H, sum);
-            if (!any)                           // also of weight 0: zeros, whatever the logits are
-                for (int g = 0; g < a.G; ++g) in[r * a.G + g] = 0;
-        }
-        if (!a.grad) {
-            __syncthreads();
-            continue;
-        }
+        decide_tile(a, t, r0, nr, given, sum);
         __syncthreads();
+        if (!a.grad) continue;
 #pragma unroll
         for (int u = 0; u < kHeadsPerThread; ++u) {
             const int h = tid + u * kThreads;
             if (h >= heads) continue;
             float *xh = x + h * k.stride;
-            if (!in[h]) {
-                for (int j = 0; j < a.V; ++j) xh[j] = 0.0f;
-                continue;
-            }
-            const float2 d = dec[a.G == 1 ? h : h / a.G];
+            const bool in = t.in[h] != 0;
+            const float2 d = t.dec[quotient(h, k.inv_g, a.G)];
             const Slope f = slope_of(v[u].m, v[u].s, le[u].x, le[u].y, d);
-            for (int j = 0; j < a.V; ++j) xh[j] = slope_at<true>(f, xh[j]);
-            xh[c[u]] += d.x;
+#pragma unroll 4
+            for (int j = 0; j < a.V; ++j) xh[j] = in ? slope_at<true>(f, xh[j]) : 0.0f;
+            if (in) xh[c[u]] += d.x;
         }
         __syncthreads();
         typename T::item *grad = static_cast<typename T::item *>(a.grad);
@@ -791,21 +922,44 @@ void launch_row(const PolicyArgs &a, const PolicyPlan &p, unsigned blocks, hipSt
     }
 }
 
+template <typename T, int HEADS>
+void launch_lane(const PolicyArgs &a, unsigned blocks, int lanes, hipStream_t s)
+{
+    const dim3 grid(blocks), block(kThreads);
+    if (a.V == 1) hipLaunchKernelGGL((policy_lane_kernel<T, 1, HEADS>), grid, block, 0, s, a, lanes);
+    else if (a.V == 2) hipLaunchKernelGGL((policy_lane_kernel<T, 2, HEADS>), grid, block, 0, s, a, lanes);
+    else if (a.V == 3) hipLaunchKernelGGL((policy_lane_kernel<T, 3, HEADS>), grid, block, 0, s, a, lanes);
+    else hipLaunchKernelGGL((policy_lane_kernel<T, 4, HEADS>), grid, block, 0, s, a, lanes);
+}
+
 template <typename T>
 hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
 {
+    if (p.lanes) {
+        const int64_t per_block = (int64_t)(kThreads / 64) * (64 / p.lanes), groups = (a.R + per_block - 1) / per_block;
+        const unsigned blocks = (unsigned)(groups < kTileBlocks ? groups : kTileBlocks);
+        if (a.R > 0) {
+            if (a.G == 1) launch_lane<T, 1>(a, blocks, p.lanes, s);
+            else if (a.G == 2) launch_lane<T, 2>(a, blocks, p.lanes, s);
+            else launch_lane<T, 4>(a, blocks, p.lanes, s);
+        }
+        return launch_terms(a, blocks, s);
+    }
     if (p.tile) {
         const int gv = a.G * a.V;
         TileShape k;
         k.per_tile = p.tile;
         k.stride = a.V | 1;
         k.inv_v = (unsigned)((((uint64_t)1 << 32) + a.V - 1) / a.V);
-        k.inv_gv = (unsigned)((((uint64_t)1 << 32) + gv - 1) / gv);
+        k.inv_g = (unsigned)((((uint64_t)1 << 32) + a.G - 1) / a.G);
         k.dense = (a.G == 1 || a.ld_g == a.V) && (a.R == 1 || a.ld_r == gv);
         k.gdense = (a.G == 1 || a.gld_g == a.V) && (a.R == 1 || a.gld_r == gv);
         const int64_t tiles = (a.R + p.tile - 1) / p.tile;
         const unsigned blocks = (unsigned)(tiles < kTileBlocks ? tiles : kTileBlocks);
-        if (a.R > 0) hipLaunchKernelGGL(policy_tile_kernel<T>, dim3(blocks), dim3(kThreads), 0, s, a, k);
+        if (a.R > 0) {
+            const dim3 grid(blocks), block(kThreads);
+            hipLaunchKernelGGL(policy_tile_kernel<T>, grid, block, 0, s, a, k);
+        }
         return launch_terms(a, blocks, s);
     }
     if (p.row) {
@@ -832,9 +986,17 @@ hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
 PolicyPlan plan_policy(int64_t R, int G, int V, int type, bool grad)
 {
     PolicyPlan p{};
+    if (V <= 4 && G <= 256) {
+        p.lanes = G <= 2 ? 1 : (G + 3) / 4;
+        p.bytes = (int64_t)kTileBlocks * kPolicySums * 8;
+        return p;
+    }
     if (V <= kTileChoices && G <= kTileHeads && (int64_t)G * (V | 1) <= kTileItems) {
         const int by_heads = kTileHeads / G, by_items = kTileItems / (G * (V | 1));
         p.tile = by_heads < by_items ? by_heads : by_items;
+        // fewer decisions a tile where that leaves compute units without one
+        const int64_t spread = (R + 2 * kUnits - 1) / (2 * kUnits);
+        if (spread < p.tile) p.tile = spread > 1 ? (int)spread : 1;
         p.bytes = (int64_t)kTileBlocks * kPolicySums * 8;
         return p;
     }
