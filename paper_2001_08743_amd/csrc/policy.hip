@@ -306,6 +306,7 @@ constexpr int kTileHeads = 1024;                // at most: kHeadsPerThread of e
 constexpr int kHeadsPerThread = kTileHeads / kThreads;
 constexpr int kTileItems = 8448;                // fp32 logits in LDS, 33 KiB: four workgroups share a compute unit
 constexpr int kTileChoices = 32;                // beyond, a tile has fewer heads than threads
+constexpr int kLaneChoices = 64;                // what a lane's registers hold
 
 struct TileShape {
     int per_tile;           // decisions of a tile
@@ -392,11 +393,50 @@ __device__ __forceinline__ float2 head_of(const PolicyArgs &a, Soft &v, float xa
     return make_float2(xa - v.m - le.x, le.y);
 }
 
-// Up to four choices: a lane holds HEADS consecutive heads of a decision, as many lanes as it takes side by side a decision, and a wave as
-// many decisions as fit (24 heads: six lanes, ten decisions).  Nothing goes through LDS and no wave waits for another.
-template <typename T, int V, int HEADS>
-__global__ void __launch_bounds__(kThreads, 4) policy_lane_kernel(const PolicyArgs a, int lanes)
+// A lane holds HEADS consecutive heads of up to VP choices in registers (four heads of up to four choices, one of up to 64); as many lanes as
+// that takes side by side are a decision, and a wave takes as many decisions as fit (24 heads of 3: six lanes, ten
+// decisions).  Nothing goes through LDS and no wave waits for another.  Choices from V to VP are masked ones.
+// V = VP is known at compile time up to four, where a lane's heads are one run of items.
+template <typename T>
+__device__ __forceinline__ void read_head(const typename T::item *p, int n, float *x, int vp)
 {
+    typedef typename T::item items __attribute__((ext_vector_type(4)));
+    typedef items loose __attribute__((aligned(sizeof(typename T::item))));
+#pragma unroll
+    for (int q = 0; q < vp; q += 4) {
+        if (q + 4 <= n) {
+            const items w = *reinterpret_cast<const loose *>(p + q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[q + j] = T::get(w[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[q + j] = q + j < n ? T::get(p[q + j]) : -__builtin_inff();
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void write_head(typename T::item *p, int n, const float *y, int vp)
+{
+    typedef typename T::item items __attribute__((ext_vector_type(4)));
+    typedef items loose __attribute__((aligned(sizeof(typename T::item))));
+#pragma unroll
+    for (int q = 0; q < vp; q += 4) {
+        if (q + 4 <= n) {
+            const items w = {T::put(y[q]), T::put(y[q + 1]), T::put(y[q + 2]), T::put(y[q + 3])};
+            *reinterpret_cast<loose *>(p + q) = w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (q + j < n) p[q + j] = T::put(y[q + j]);
+        }
+    }
+}
+
+template <typename T, int VP, int HEADS>
+__global__ void __launch_bounds__(kThreads, VP > 32 ? 2 : VP > 16 ? 3 : 4) policy_lane_kernel(const PolicyArgs a, int lanes)
+{
+    constexpr bool kExact = VP <= 4;
+    const int V = kExact ? VP : a.V;
     const int lane = threadIdx.x & 63, per_wave = 64 / lanes, mine = lane / lanes, part = lane - mine * lanes;
     const int64_t step = (int64_t)gridDim.x * (kThreads / 64) * per_wave;
     const int h0 = part * HEADS, n = mine < per_wave ? (a.G - h0 < HEADS ? a.G - h0 : HEADS) : 0;      // heads of this lane
@@ -405,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, 4) policy_lane_kernel(const PolicyAr
     for (int64_t r0 = ((int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * per_wave; r0 < a.R; r0 += step) {
         const int64_t r = r0 + mine;
         const int here = r < a.R ? n : 0;
-        float x[HEADS][V];
+        float x[HEADS][VP];
         int c[HEADS];
         Given given{};
         bool on = false;
@@ -413,22 +453,24 @@ __global__ void __launch_bounds__(kThreads, 4) policy_lane_kernel(const PolicyAr
         for (int u = 0; u < HEADS; ++u) {
             c[u] = -1;
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[u][j] = 0.0f;
+            for (int j = 0; j < VP; ++j) x[u][j] = 0.0f;
         }
         if (here > 0) {
             const typename T::item *p = static_cast<const typename T::item *>(a.logits) + r * a.ld_r + h0 * a.ld_g;
-            if (dense) {
-                typename T::item y[HEADS * V];
+            if (!kExact) {
+                read_head<T>(p, V, x[0], VP);
+            } else if (dense) {
+                typename T::item y[HEADS * VP];
 #pragma unroll
-                for (int i = 0; i < HEADS * V; ++i) y[i] = p[i];
+                for (int i = 0; i < HEADS * VP; ++i) y[i] = p[i];
 #pragma unroll
-                for (int i = 0; i < HEADS * V; ++i) x[i / V][i % V] = T::get(y[i]);
+                for (int i = 0; i < HEADS * VP; ++i) x[i / VP][i % VP] = T::get(y[i]);
             } else {
 #pragma unroll
                 for (int u = 0; u < HEADS; ++u)
                     if (u < here)
 #pragma unroll
-                        for (int j = 0; j < V; ++j) x[u][j] = T::get(p[u * a.ld_g + j]);
+                        for (int j = 0; j < VP; ++j) x[u][j] = T::get(p[u * a.ld_g + j]);
             }
 #pragma unroll
             for (int u = 0; u < HEADS; ++u)
@@ -446,13 +488,13 @@ __global__ void __launch_bounds__(kThreads, 4) policy_lane_kernel(const PolicyAr
             le[u] = make_float2(0.0f, 0.0f);
             float xa = 0.0f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
+            for (int j = 0; j < VP; ++j) {
                 v[u].m = fmaxf(v[u].m, x[u][j]);
                 xa = j == c[u] ? x[u][j] : xa;
             }
             const Scale k2 = scale_of(v[u].m);
 #pragma unroll
-            for (int j = 0; j < V; ++j) soft_add(v[u], x[u][j], k2);
+            for (int j = 0; j < VP; ++j) soft_add(v[u], x[u][j], k2);
             const float2 one = head_of(a, v[u], xa, c[u], le[u]);
             lp += (double)one.x;
             H += (double)one.y;
@@ -477,23 +519,24 @@ __global__ void __launch_bounds__(kThreads, 4) policy_lane_kernel(const PolicyAr
         on = __shfl((int)on, first);
         if (here == 0) continue;
         typename T::item *p = static_cast<typename T::item *>(a.grad) + r * a.gld_r + h0 * a.gld_g;
-        typename T::item y[HEADS * V];
 #pragma unroll
         for (int u = 0; u < HEADS; ++u) {
             const bool in = on && c[u] >= 0;
             const Slope f = slope_of(v[u].m, v[u].s, le[u].x, le[u].y, d);
 #pragma unroll
-            for (int j = 0; j < V; ++j) y[u * V + j] = T::put(in ? slope_at<true>(f, x[u][j]) + (j == c[u] ? d.x : 0.0f) : 0.0f);
+            for (int j = 0; j < VP; ++j) x[u][j] = in ? slope_at<true>(f, x[u][j]) + (j == c[u] ? d.x : 0.0f) : 0.0f;
         }
-        if (gdense) {
+        if (!kExact) {
+            write_head<T>(p, V, x[0], VP);
+        } else if (gdense) {
 #pragma unroll
-            for (int i = 0; i < HEADS * V; ++i) p[i] = y[i];
+            for (int i = 0; i < HEADS * VP; ++i) p[i] = T::put(x[i / VP][i % VP]);
         } else {
 #pragma unroll
             for (int u = 0; u < HEADS; ++u)
                 if (u < here)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) p[u * a.gld_g + j] = y[u * V + j];
+                    for (int j = 0; j < VP; ++j) p[u * a.gld_g + j] = T::put(x[u][j]);
         }
     }
     if (a.old_logp) store_sums<kThreads / 64>(a, sum);
@@ -753,13 +796,16 @@ __global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_w
 
 // --- any number of heads and choices, in three steps: sums of parts of heads, decisions, gradient
 
-template <typename T>
+// THREADS of a part: a wave of short heads, a workgroup of parts of long ones.
+template <typename T, int THREADS>
 __global__ void __launch_bounds__(kThreads) policy_part_kernel(const PolicyArgs a, int splits, int chunk)
 {
+    constexpr int kParts = kThreads / THREADS;
     __shared__ Soft lds[kThreads / 64];
+    const int tid = threadIdx.x % THREADS, group = THREADS == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
     const int64_t units = a.R * a.G * splits;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int64_t h = u / splits, r = h / a.G;
+    for (int64_t u = (int64_t)blockIdx.x * kParts + group; u < units; u += (int64_t)gridDim.x * kParts) {
+        const int64_t h = splits == 1 ? u : u / splits, r = a.G == 1 ? h : h / a.G;
         if (!counts(a, r)) continue;
         const int c = choice_of(a, h);
         if (c < 0 || c == a.V) continue;
@@ -770,27 +816,46 @@ __global__ void __launch_bounds__(kThreads) policy_part_kernel(const PolicyArgs 
         const int head = (int)items_to_boundary<T>(row + lo, hi - lo), n_vec = (hi - lo - head) / T::kVec, tail = lo + head + n_vec * T::kVec;
         const uint4 *body = reinterpret_cast<const uint4 *>(row + lo + head);
         float end[2] = {-__builtin_inff(), -__builtin_inff()};
-        if ((int)threadIdx.x < head) end[0] = T::get(row[lo + threadIdx.x]);
-        if ((int)threadIdx.x < hi - tail) end[1] = T::get(row[tail + threadIdx.x]);
+        if (tid < head) end[0] = T::get(row[lo + tid]);
+        if (tid < hi - tail) end[1] = T::get(row[tail + tid]);
         Scale k2 = scale_of(v.m);
         soft_add_all(v, k2, end);
-        for (int i = threadIdx.x; i < n_vec; i += kThreads) {
+        for (int i = tid; i < n_vec; i += THREADS) {
             float x[T::kVec];
             T::unpack(body[i], x);
             soft_add_all(v, k2, x);
         }
         v = soft_wave(v);
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 1; w < kThreads / 64; ++w) v = soft_join(v, lds[w]);
-            reinterpret_cast<float4 *>(a.part)[u] = make_float4(v.m, v.s, v.t, 0.0f);
+        if (THREADS > 64) {
+            if ((tid & 63) == 0) lds[tid >> 6] = v;
+            __syncthreads();
+            if (tid == 0)
+                for (int w = 1; w < THREADS / 64; ++w) v = soft_join(v, lds[w]);
         }
-        __syncthreads();
+        if (tid == 0) reinterpret_cast<float4 *>(a.part)[u] = make_float4(v.m, v.s, v.t, 0.0f);
+        if (THREADS > 64) __syncthreads();
     }
 }
 
-// A wave per decision: its heads one after the other, the parts of a head over the lanes.
+// A head of a decision from the sums of its parts: what it adds to the decision, and what its gradient needs.
+template <typename T>
+__device__ __forceinline__ float4 join_head(const PolicyArgs &a, int64_t r, int g, int c, const Soft &v, double &lp, double &H, bool &in)
+{
+    if (c == a.V) {
+        lp = H = __builtin_nan("");
+        in = true;
+        return make_float4(0.0f, __builtin_nanf(""), 0.0f, __int_as_float(0));
+    }
+    if (c < 0 || v.s == 0.0f) return make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));       // 0: every choice is masked
+    const float2 le = log_and_entropy(v);
+    const float x = T::get(static_cast<const typename T::item *>(a.logits)[r * a.ld_r + g * a.ld_g + c]);
+    lp += (double)x - (double)v.m - (double)le.x;
+    H += (double)le.y;
+    in = true;
+    return make_float4(v.m, v.s, le.y, __int_as_float(c));
+}
+
+// A wave per decision.  Heads of one part: a lane each; of several: the heads one after the other, their parts over the lanes.
 template <typename T, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64) policy_join_kernel(const PolicyArgs a, int splits)
 {
@@ -800,31 +865,36 @@ __global__ void __launch_bounds__(WAVES * 64) policy_join_kernel(const PolicyArg
         double lp = 0.0, H = 0.0;
         bool in = false;
         if (counts(a, r)) {
-            for (int g = 0; g < a.G; ++g) {
-                const int64_t h = r * a.G + g;
-                const int c = choice_of(a, h);
-                float4 out = make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
-                if (c == a.V) {
-                    lp = H = __builtin_nan("");
-                    out = make_float4(0.0f, __builtin_nanf(""), 0.0f, __int_as_float(0));
-                    in = true;
-                } else if (c >= 0) {
+            if (splits == 1) {
+                for (int g = lane; g < a.G; g += 64) {
+                    const int64_t h = r * a.G + g;
+                    const int c = choice_of(a, h);
                     Soft v = soft_none();
-                    for (int i = lane; i < splits; i += 64) {
-                        const float4 p = reinterpret_cast<const float4 *>(a.part)[h * splits + i];
-                        v = soft_join(v, {p.x, p.y, p.z});
+                    if (c >= 0 && c < a.V) {
+                        const float4 p = reinterpret_cast<const float4 *>(a.part)[h];
+                        v = {p.x, p.y, p.z};
                     }
-                    v = soft_wave(v);
-                    if (v.s != 0.0f) {                     // 0: every choice is masked
-                        const float2 le = log_and_entropy(v);
-                        const float x = T::get(static_cast<const typename T::item *>(a.logits)[r * a.ld_r + g * a.ld_g + c]);
-                        lp += (double)x - (double)v.m - (double)le.x;
-                        H += (double)le.y;
-                        out = make_float4(v.m, v.s, le.y, __int_as_float(c));
-                        in = true;
-                    }
+                    const float4 out = join_head<T>(a, r, g, c, v, lp, H, in);
+                    if (a.grad) a.head[h] = out;
                 }
-                if (a.grad && lane == 0) a.head[h] = out;
+                lp = wave_sum(lp);
+                H = wave_sum(H);
+                in = __any(in);
+            } else {
+                for (int g = 0; g < a.G; ++g) {
+                    const int64_t h = r * a.G + g;
+                    const int c = choice_of(a, h);
+                    Soft v = soft_none();
+                    if (c >= 0 && c < a.V) {
+                        for (int i = lane; i < splits; i += 64) {
+                            const float4 p = reinterpret_cast<const float4 *>(a.part)[h * splits + i];
+                            v = soft_join(v, {p.x, p.y, p.z});
+                        }
+                        v = soft_wave(v);
+                    }
+                    const float4 out = join_head<T>(a, r, g, c, v, lp, H, in);
+                    if (a.grad && lane == 0) a.head[h] = out;
+                }
             }
         }
         if (lane == 0) {
@@ -835,19 +905,21 @@ __global__ void __launch_bounds__(WAVES * 64) policy_join_kernel(const PolicyArg
     if (a.old_logp) store_sums<WAVES>(a, sum);
 }
 
-template <typename T>
+template <typename T, int THREADS>
 __global__ void __launch_bounds__(kThreads) policy_grad_kernel(const PolicyArgs a, int splits, int chunk)
 {
+    constexpr int kParts = kThreads / THREADS;
+    const int tid = threadIdx.x % THREADS, group = THREADS == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
     const int64_t units = a.R * a.G * splits;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int64_t h = u / splits, r = h / a.G;
+    for (int64_t u = (int64_t)blockIdx.x * kParts + group; u < units; u += (int64_t)gridDim.x * kParts) {
+        const int64_t h = splits == 1 ? u : u / splits, r = a.G == 1 ? h : h / a.G;
         const int g = (int)(h - r * a.G), lo = (int)(u - h * splits) * chunk;
         const int hi = lo + chunk < a.V ? lo + chunk : a.V;
         typename T::item *to = static_cast<typename T::item *>(a.grad) + r * a.gld_r + g * a.gld_g;
         const float4 k = counts(a, r) ? a.head[h] : make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
         const int c = __float_as_int(k.w);
         if (c < 0) {
-            for (int v = lo + threadIdx.x; v < hi; v += kThreads) to[v] = T::put(0.0f);
+            for (int v = lo + tid; v < hi; v += THREADS) to[v] = T::put(0.0f);
             continue;
         }
         const float2 d = a.dec[r];
@@ -855,9 +927,9 @@ __global__ void __launch_bounds__(kThreads) policy_grad_kernel(const PolicyArgs 
         const Slope f = slope_of(k.x, k.y, logf(k.y), k.z, d);
         const int head = (int)items_to_boundary<T>(row + lo, hi - lo), n_vec = (hi - lo - head) / T::kVec, tail = lo + head + n_vec * T::kVec;
         auto one = [&](int v) { to[v] = T::put(slope_at<true>(f, T::get(row[v])) + (v == c ? d.x : 0.0f)); };
-        if ((int)threadIdx.x < head) one(lo + threadIdx.x);
-        if ((int)threadIdx.x < hi - tail) one(tail + threadIdx.x);
-        for (int i = threadIdx.x; i < n_vec; i += kThreads) {
+        if (tid < head) one(lo + tid);
+        if (tid < hi - tail) one(tail + tid);
+        for (int i = tid; i < n_vec; i += THREADS) {
             const int at = lo + head + i * T::kVec;
             float x[T::kVec];
             T::unpack(*reinterpret_cast<const uint4 *>(row + at), x);
@@ -872,6 +944,7 @@ constexpr int kJoinBlocks = 1024;
 constexpr int kTileBlocks = 1024;               // what is on the chip at a time
 constexpr int kUnits = 256;                     // compute units
 constexpr int kRowBlocks = 6 * kUnits;
+constexpr int kWaveChunk = 2048;                // choices of a part that a wave takes
 constexpr int kJoinFew = 16;                    // decisions that one workgroup joins, a wave each
 
 // A wave or a workgroup per row, by its pieces of 16 bytes: 64 threads up to 1024 pieces (four rows a workgroup, no barrier), 256 up to
@@ -931,6 +1004,18 @@ void launch_lane(const PolicyArgs &a, unsigned blocks, int lanes, hipStream_t s)
     else if (a.V == 3) hipLaunchKernelGGL((policy_lane_kernel<T, 3, HEADS>), grid, block, 0, s, a, lanes);
     else hipLaunchKernelGGL((policy_lane_kernel<T, 4, HEADS>), grid, block, 0, s, a, lanes);
 }
+template <typename T>
+void launch_lane_of(const PolicyArgs &a, unsigned blocks, int lanes, hipStream_t s)
+{
+    const dim3 grid(blocks), block(kThreads);
+    if (a.V > 32) hipLaunchKernelGGL((policy_lane_kernel<T, 64, 1>), grid, block, 0, s, a, lanes);
+    else if (a.V > 16) hipLaunchKernelGGL((policy_lane_kernel<T, 32, 1>), grid, block, 0, s, a, lanes);
+    else if (a.V > 8) hipLaunchKernelGGL((policy_lane_kernel<T, 16, 1>), grid, block, 0, s, a, lanes);
+    else if (a.V > 4) hipLaunchKernelGGL((policy_lane_kernel<T, 8, 1>), grid, block, 0, s, a, lanes);
+    else if (a.G == 1) launch_lane<T, 1>(a, blocks, lanes, s);
+    else if (a.G == 2) launch_lane<T, 2>(a, blocks, lanes, s);
+    else launch_lane<T, 4>(a, blocks, lanes, s);
+}
 
 template <typename T>
 hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
@@ -938,11 +1023,7 @@ hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
     if (p.lanes) {
         const int64_t per_block = (int64_t)(kThreads / 64) * (64 / p.lanes), groups = (a.R + per_block - 1) / per_block;
         const unsigned blocks = (unsigned)(groups < kTileBlocks ? groups : kTileBlocks);
-        if (a.R > 0) {
-            if (a.G == 1) launch_lane<T, 1>(a, blocks, p.lanes, s);
-            else if (a.G == 2) launch_lane<T, 2>(a, blocks, p.lanes, s);
-            else launch_lane<T, 4>(a, blocks, p.lanes, s);
-        }
+        if (a.R > 0) launch_lane_of<T>(a, blocks, p.lanes, s);
         return launch_terms(a, blocks, s);
     }
     if (p.tile) {
@@ -973,10 +1054,14 @@ hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
     const int64_t units = a.R * a.G * p.splits;
     const unsigned join = (unsigned)(a.R <= kJoinFew ? 1 : (a.R + 3) / 4 < kJoinBlocks ? (a.R + 3) / 4 : kJoinBlocks);
     if (a.R > 0) {
-        hipLaunchKernelGGL(policy_part_kernel<T>, dim3(blocks_for(units)), dim3(kThreads), 0, s, a, p.splits, p.chunk);
+        const bool wave = p.chunk <= kWaveChunk;
+        const dim3 grid(blocks_for(wave ? (units + 3) / 4 : units));
+        if (wave) hipLaunchKernelGGL((policy_part_kernel<T, 64>), grid, dim3(kThreads), 0, s, a, p.splits, p.chunk);
+        else hipLaunchKernelGGL((policy_part_kernel<T, kThreads>), grid, dim3(kThreads), 0, s, a, p.splits, p.chunk);
         if (join == 1) hipLaunchKernelGGL((policy_join_kernel<T, kJoinFew>), dim3(1), dim3(kJoinFew * 64), 0, s, a, p.splits);
         else hipLaunchKernelGGL((policy_join_kernel<T, kThreads / 64>), dim3(join), dim3(kThreads), 0, s, a, p.splits);
-        if (a.grad) hipLaunchKernelGGL(policy_grad_kernel<T>, dim3(blocks_for(units)), dim3(kThreads), 0, s, a, p.splits, p.chunk);
+        if (a.grad && wave) hipLaunchKernelGGL((policy_grad_kernel<T, 64>), grid, dim3(kThreads), 0, s, a, p.splits, p.chunk);
+        else if (a.grad) hipLaunchKernelGGL((policy_grad_kernel<T, kThreads>), grid, dim3(kThreads), 0, s, a, p.splits, p.chunk);
     }
     return launch_terms(a, join, s);
 }
@@ -986,8 +1071,8 @@ hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
 PolicyPlan plan_policy(int64_t R, int G, int V, int type, bool grad)
 {
     PolicyPlan p{};
-    if (V <= 4 && G <= 256) {
-        p.lanes = G <= 2 ? 1 : (G + 3) / 4;
+    if (V <= 4 ? G <= 256 : V <= kLaneChoices && G <= 64 && (G > 1 || V <= 32)) {
+        p.lanes = V > 4 ? G : G <= 2 ? 1 : (G + 3) / 4;
         p.bytes = (int64_t)kTileBlocks * kPolicySums * 8;
         return p;
     }
