@@ -662,19 +662,28 @@ def cham_policy_loss(logits, actions, old_logp, advantages, first_action: int = 
         if grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != dev:
             raise ChamError(f"grad_logits: need {logits.dtype} {tuple(logits.shape)} on {dev}, got {grad.dtype} {tuple(grad.shape)} on {grad.device}")
         _, _, _, gld_r, gld_g = _heads(grad, "grad_logits")
-    coef = _PolicyCoef(clip_low, clip_high, value_coef, entropy_coef, kl_coef, value_clip)
-    workspace, at = _scratch(workspace, dev, cham_policy_workspace_bytes, R, G, V, code, grad is not None)
     row = (R,)
+    rows = (weights, old_logp, advantages, ref_logp, values, old_values, returns, out.get("logp"), out.get("entropy"),
+            out.get("grad_values") if want_grad else None)
+    at = []
+    for i, t in enumerate(rows):                        # as _addr, ten of them a call
+        if t is None:
+            at.append(None)
+        elif t.dtype is f32 and t.shape == row and t.device == dev and t.is_contiguous():
+            at.append(t.data_ptr())
+        else:
+            _addr(t, dev, _LOSS_ROWS[i], f32, row)
+    coef = _PolicyCoef(clip_low, clip_high, value_coef, entropy_coef, kl_coef, value_clip)
+    workspace, ws = _scratch(workspace, dev, cham_policy_workspace_bytes, R, G, V, code, grad is not None)
     _check(load().cham_policy_loss(
-        logits.data_ptr(), code, R, G, V, ld_r, ld_g, acts, _type_of(actions, _ACTION_TYPES, "actions"), first_action,
-        _addr(weights, dev, "weights", f32, row), _addr(old_logp, dev, "old_logp", f32, row), _addr(advantages, dev, "advantages", f32, row),
-        _addr(ref_logp, dev, "ref_logp", f32, row), _addr(values, dev, "values", f32, row), _addr(old_values, dev, "old_values", f32, row),
-        _addr(returns, dev, "returns", f32, row), C.byref(coef), _addr(out["terms"], dev, "terms", f32, (len(TERMS),)),
-        _addr(out.get("logp"), dev, "logp", f32, row), _addr(out.get("entropy"), dev, "entropy", f32, row),
-        None if grad is None else grad.data_ptr(), gld_r, gld_g,
-        _addr(out.get("grad_values"), dev, "grad_values", f32, row) if want_grad else None, at, workspace.numel(), stream))
+        logits.data_ptr(), code, R, G, V, ld_r, ld_g, acts, _type_of(actions, _ACTION_TYPES, "actions"), first_action, *at[:7], coef,
+        _addr(out["terms"], dev, "terms", f32, (len(TERMS),)), at[7], at[8], None if grad is None else grad.data_ptr(), gld_r, gld_g, at[9],
+        ws, workspace.numel(), stream))
     out["workspace"] = workspace
     return out
+
+
+_LOSS_ROWS = ("weights", "old_logp", "advantages", "ref_logp", "values", "old_values", "returns", "logp", "entropy", "grad_values")
 
 
 def _matrix(t, device, what: str, dtype, shape):
@@ -743,6 +752,7 @@ class GradList:
         self.ptrs = (C.c_void_p * max(n, 1))(*[t.data_ptr() for t in self.tensors])
         self.numels = (C.c_int64 * max(n, 1))(*[t.numel() for t in self.tensors])
         self.types = (C.c_int32 * max(n, 1))(*codes)
+        self.sizes = bytes(self.numels) + bytes(self.types)
         self.workspace_bytes = _check(load().cham_grad_workspace_bytes(self.numels, self.types, n))
 
 
@@ -777,7 +787,7 @@ def cham_clip_grads(grads, max_norm: float, out=None, norm=None, norm_given: boo
     outs = None
     if out is not None:
         out = out if isinstance(out, GradList) else GradList(out)
-        if out.n != grads.n or (out.n and out.device != grads.device) or bytes(out.numels) != bytes(grads.numels) or bytes(out.types) != bytes(grads.types):
+        if out.sizes != grads.sizes or (out.n and out.device != grads.device):
             raise ChamError("out: need tensors of the same sizes, types and device as the gradients")
         outs = out.ptrs
     _check(load().cham_clip_grads(grads.ptrs, outs, grads.numels, grads.types, grads.n, max_norm, norm_at, at, workspace.numel(),

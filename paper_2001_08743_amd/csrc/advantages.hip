@@ -80,13 +80,25 @@ __device__ __forceinline__ Steps load_steps(const GaeArgs &a, int64_t b, int64_t
         }
         return s;
     }
+    // everything asked for before anything is looked at
+    typename T::item r[kSteps], v[kSteps];
+    uint8_t d[kSteps];
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
+    for (int i = 0; i < kSteps; ++i) {
+        r[i] = v[i] = T::put(0.0f);
+        d[i] = 0;
         if (i >= s.first && i < s.end) {
-            s.r[i] = T::get(rew[i * a.r_lds]);
-            s.v[i] = T::get(val[i * a.v_lds]);
-            if (done && done[i * a.d_lds]) s.done |= 1u << i;
+            r[i] = rew[i * a.r_lds];
+            v[i] = val[i * a.v_lds];
+            if (done) d[i] = done[i * a.d_lds];
         }
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        s.r[i] = T::get(r[i]);
+        s.v[i] = T::get(v[i]);
+        s.done |= d[i] != 0 ? 1u << i : 0u;
+    }
     return s;
 }
 

@@ -837,9 +837,8 @@ __global__ void __launch_bounds__(kThreads) policy_part_kernel(const PolicyArgs 
     }
 }
 
-// A head of a decision from the sums of its parts: what it adds to the decision, and what its gradient needs.
-template <typename T>
-__device__ __forceinline__ float4 join_head(const PolicyArgs &a, int64_t r, int g, int c, const Soft &v, double &lp, double &H, bool &in)
+// A head of a decision from the sums of its parts and its action's logit x: what it adds to the decision, and what its gradient needs.
+__device__ __forceinline__ float4 join_head(const PolicyArgs &a, int c, float x, const Soft &v, double &lp, double &H, bool &in)
 {
     if (c == a.V) {
         lp = H = __builtin_nan("");
@@ -848,7 +847,6 @@ __device__ __forceinline__ float4 join_head(const PolicyArgs &a, int64_t r, int 
     }
     if (c < 0 || v.s == 0.0f) return make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));       // 0: every choice is masked
     const float2 le = log_and_entropy(v);
-    const float x = T::get(static_cast<const typename T::item *>(a.logits)[r * a.ld_r + g * a.ld_g + c]);
     lp += (double)x - (double)v.m - (double)le.x;
     H += (double)le.y;
     in = true;
@@ -864,17 +862,20 @@ __global__ void __launch_bounds__(WAVES * 64) policy_join_kernel(const PolicyArg
     for (int64_t r = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6); r < a.R; r += (int64_t)gridDim.x * WAVES) {
         double lp = 0.0, H = 0.0;
         bool in = false;
+        const Given given = given_of(a, r, load_plain);        // asked for ahead of the sums
         if (counts(a, r)) {
             if (splits == 1) {
                 for (int g = lane; g < a.G; g += 64) {
                     const int64_t h = r * a.G + g;
                     const int c = choice_of(a, h);
                     Soft v = soft_none();
+                    float x = 0.0f;
                     if (c >= 0 && c < a.V) {
                         const float4 p = reinterpret_cast<const float4 *>(a.part)[h];
+                        x = T::get(static_cast<const typename T::item *>(a.logits)[r * a.ld_r + g * a.ld_g + c]);
                         v = {p.x, p.y, p.z};
                     }
-                    const float4 out = join_head<T>(a, r, g, c, v, lp, H, in);
+                    const float4 out = join_head(a, c, x, v, lp, H, in);
                     if (a.grad) a.head[h] = out;
                 }
                 lp = wave_sum(lp);
@@ -885,20 +886,22 @@ __global__ void __launch_bounds__(WAVES * 64) policy_join_kernel(const PolicyArg
                     const int64_t h = r * a.G + g;
                     const int c = choice_of(a, h);
                     Soft v = soft_none();
+                    float x = 0.0f;
                     if (c >= 0 && c < a.V) {
+                        x = T::get(static_cast<const typename T::item *>(a.logits)[r * a.ld_r + g * a.ld_g + c]);
                         for (int i = lane; i < splits; i += 64) {
                             const float4 p = reinterpret_cast<const float4 *>(a.part)[h * splits + i];
                             v = soft_join(v, {p.x, p.y, p.z});
                         }
                         v = soft_wave(v);
                     }
-                    const float4 out = join_head<T>(a, r, g, c, v, lp, H, in);
+                    const float4 out = join_head(a, c, x, v, lp, H, in);
                     if (a.grad && lane == 0) a.head[h] = out;
                 }
             }
         }
         if (lane == 0) {
-            const float2 d = decide(a, r, given_of(a, r, load_plain), in, lp, H, sum);
+            const float2 d = decide(a, r, given, in, lp, H, sum);
             if (a.grad) a.dec[r] = d;
         }
     }
