@@ -28,14 +28,15 @@ __device__ __forceinline__ int64_t length_of(const GaeArgs &a, int64_t b)
     return n < 0 ? 0 : n < a.S ? n : a.S;
 }
 
-// Eight steps of a thread: rewards, values, dones, and the value behind them.  Those outside [first, end) are none and do nothing; behind
-// step `boot_at` comes the bootstrap.
+// Eight steps of a thread from `base` on; those at and behind `end` are none.
 struct Steps {
-    float r[kSteps], v[kSteps], next, boot;
+    float v[kSteps];
+    double d[kSteps];                     // b_t
     uint32_t done;                        // a bit each
-    int first, end, boot_at;
+    int end;
 };
 
+// Items base .. base + 7 of a row, and of its dones.
 template <typename T>
 __device__ __forceinline__ void load_eight(const typename T::item *p, float (&x)[kSteps])
 {
@@ -48,122 +49,145 @@ __device__ __forceinline__ void load_eight(const typename T::item *p, float (&x)
         for (int j = 0; j < T::kVec; ++j) x[k * T::kVec + j] = y[j];
     }
 }
+__device__ __forceinline__ uint32_t load_dones(const uint8_t *p)
+{
+    typedef unsigned words __attribute__((ext_vector_type(2), aligned(1)));
+    const words w = *reinterpret_cast<const words *>(p);
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) bits |= (((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 0xffu) != 0 ? 1u << i : 0u;
+    return bits;
+}
 
-__device__ __forceinline__ int within(int64_t x) { return x < 0 ? 0 : x > kSteps ? kSteps : (int)x; }
-
-// Steps [base, base + 8) of trajectory b as far as they are in [lo, hi), hi at most its length.
-template <typename T, bool DENSE>
-__device__ __forceinline__ Steps load_steps(const GaeArgs &a, int64_t b, int64_t base, int64_t lo, int64_t hi, int64_t len)
+// Steps [base, base + 8) of trajectory b as far as they are below `top`, at most its length.  Steps that are not there have b_t = 0: they
+// stand behind the last one, where the advantage is 0, so their factor does not matter.
+template <typename T, bool DENSE, bool DONES>
+__device__ __forceinline__ Steps load_steps(const GaeArgs &a, int64_t b, int64_t base, int64_t top, int64_t len)
 {
     Steps s;
-    s.first = within(lo - base);
-    s.end = within(hi - base);
-    s.boot_at = len - 1 - base >= 0 && len - 1 - base < kSteps ? (int)(len - 1 - base) : -1;
+    const int64_t left = top - base;
+    s.end = left < 0 ? 0 : left > kSteps ? kSteps : (int)left;
     s.done = 0;
-    s.next = s.boot = 0.0f;
+    float r[kSteps], next = 0.0f, boot = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) s.r[i] = s.v[i] = 0.0f;
-    if (s.first >= s.end) return s;
-    const typename T::item *rew = static_cast<const typename T::item *>(a.rewards) + b * a.r_ldb + base * a.r_lds;
-    const typename T::item *val = static_cast<const typename T::item *>(a.values) + b * a.v_ldb + base * a.v_lds;
-    const uint8_t *done = a.dones ? a.dones + b * a.d_ldb + base * a.d_lds : nullptr;
-    if (base + kSteps < len) s.next = T::get(val[kSteps * a.v_lds]);
-    if (s.boot_at >= 0 && a.bootstrap) s.boot = a.bootstrap[b];
-    if (DENSE && s.first == 0 && s.end == kSteps) {
-        load_eight<T>(rew, s.r);
-        load_eight<T>(val, s.v);
-        if (done) {
-            typedef unsigned words __attribute__((ext_vector_type(2), aligned(1)));
-            const words w = *reinterpret_cast<const words *>(done);
+    for (int i = 0; i < kSteps; ++i) r[i] = s.v[i] = 0.0f;
+    int boot_at = -1;
+    if (s.end > 0) {
+        const typename T::item *rew = static_cast<const typename T::item *>(a.rewards) + b * a.r_ldb + base * a.r_lds;
+        const typename T::item *val = static_cast<const typename T::item *>(a.values) + b * a.v_ldb + base * a.v_lds;
+        const uint8_t *done = DONES ? a.dones + b * a.d_ldb + base * a.d_lds : nullptr;
+        if (base + kSteps < len) next = T::get(val[kSteps * a.v_lds]);
+        else boot_at = (int)(len - 1 - base);
+        if (boot_at >= 0 && a.bootstrap) boot = a.bootstrap[b];
+        if (s.end == kSteps) {
+            if (DENSE) {
+                load_eight<T>(rew, r);
+                load_eight<T>(val, s.v);
+                if (DONES) s.done = load_dones(done);
+            } else {
+                typename T::item x[kSteps], y[kSteps];
+                uint8_t z[kSteps];
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) s.done |= (((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 0xffu) != 0 ? 1u << i : 0u;
+                for (int i = 0; i < kSteps; ++i) {
+                    x[i] = rew[i * a.r_lds];
+                    y[i] = val[i * a.v_lds];
+                    z[i] = DONES ? done[i * a.d_lds] : 0;
+                }
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    r[i] = T::get(x[i]);
+                    s.v[i] = T::get(y[i]);
+                    s.done |= z[i] != 0 ? 1u << i : 0u;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kSteps - 1; ++i)
+                if (i < s.end) {
+                    r[i] = T::get(rew[i * a.r_lds]);
+                    s.v[i] = T::get(val[i * a.v_lds]);
+                    if (DONES && done[i * a.d_lds]) s.done |= 1u << i;
+                }
         }
-        return s;
     }
-    // everything asked for before anything is looked at
-    typename T::item r[kSteps], v[kSteps];
-    uint8_t d[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        r[i] = v[i] = T::put(0.0f);
-        d[i] = 0;
-        if (i >= s.first && i < s.end) {
-            r[i] = rew[i * a.r_lds];
-            v[i] = val[i * a.v_lds];
-            if (done) d[i] = done[i * a.d_lds];
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-        s.r[i] = T::get(r[i]);
-        s.v[i] = T::get(v[i]);
-        s.done |= d[i] != 0 ? 1u << i : 0u;
+        float n = i + 1 < kSteps ? s.v[i + 1 < kSteps ? i + 1 : i] : next;
+        n = i == boot_at ? boot : n;
+        if (DONES) n = (s.done >> i) & 1 ? 0.0f : n;
+        s.d[i] = __builtin_fma(a.gamma, (double)n, (double)r[i] - (double)s.v[i]);
     }
     return s;
 }
 
-// What step i does to the advantage behind it.
-__device__ __forceinline__ Run step_of(const GaeArgs &a, const Steps &s, int i)
-{
-    const float next = i == s.boot_at ? s.boot : i == kSteps - 1 ? s.next : s.v[i + 1 < kSteps ? i + 1 : i];
-    const bool in = i >= s.first && i < s.end, done = (s.done >> i) & 1;
-    const double d = __builtin_fma(done ? 0.0 : a.gamma, (double)next, (double)s.r[i] - (double)s.v[i]);
-    return {in ? (done ? 0.0 : a.gamma_lambda) : 1.0, in ? d : 0.0};
-}
+template <bool DONES>
+__device__ __forceinline__ double factor_of(const GaeArgs &a, const Steps &s, int i) { return DONES && (s.done >> i) & 1 ? 0.0 : a.gamma_lambda; }
+
+template <bool DONES>
 __device__ __forceinline__ Run fold(const GaeArgs &a, const Steps &s)
 {
-    Run r = step_of(a, s, kSteps - 1);
+    Run r{DONES ? factor_of<DONES>(a, s, kSteps - 1) : a.factor_eight, s.d[kSteps - 1]};
 #pragma unroll
-    for (int i = kSteps - 2; i >= 0; --i) r = run_join(step_of(a, s, i), r);
+    for (int i = kSteps - 2; i >= 0; --i) {
+        const double c = factor_of<DONES>(a, s, i);
+        if (DONES) r.p *= c;
+        r.q = __builtin_fma(c, r.q, s.d[i]);
+    }
     return r;
 }
-template <bool DENSE>
+template <bool DENSE, bool DONES>
 __device__ __forceinline__ void store_steps(const GaeArgs &a, int64_t b, const Steps &s, int64_t base, double behind)
 {
     float adv[kSteps], ret[kSteps];
 #pragma unroll
     for (int i = kSteps - 1; i >= 0; --i) {
-        const Run m = step_of(a, s, i);
-        behind = __builtin_fma(m.p, behind, m.q);
+        behind = __builtin_fma(factor_of<DONES>(a, s, i), behind, s.d[i]);
         adv[i] = (float)behind;
         ret[i] = (float)(behind + (double)s.v[i]);
     }
     const int64_t at = b * a.o_ldb + base * a.o_lds;
-    if (DENSE && s.first == 0 && s.end == kSteps) {
-        typedef float words __attribute__((ext_vector_type(4), aligned(4)));
+    if (s.end == kSteps) {
+        if (DENSE) {
+            typedef float words __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-        for (int i = 0; i < kSteps; i += 4) {
-            *reinterpret_cast<words *>(a.adv + at + i) = words{adv[i], adv[i + 1], adv[i + 2], adv[i + 3]};
-            if (a.ret) *reinterpret_cast<words *>(a.ret + at + i) = words{ret[i], ret[i + 1], ret[i + 2], ret[i + 3]};
+            for (int i = 0; i < kSteps; i += 4) {
+                *reinterpret_cast<words *>(a.adv + at + i) = words{adv[i], adv[i + 1], adv[i + 2], adv[i + 3]};
+                if (a.ret) *reinterpret_cast<words *>(a.ret + at + i) = words{ret[i], ret[i + 1], ret[i + 2], ret[i + 3]};
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) a.adv[at + i * a.o_lds] = adv[i];
+            if (a.ret)
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) a.ret[at + i * a.o_lds] = ret[i];
         }
         return;
     }
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
-        if (i >= s.first && i < s.end) {
+    for (int i = 0; i < kSteps - 1; ++i)
+        if (i < s.end) {
             a.adv[at + i * a.o_lds] = adv[i];
             if (a.ret) a.ret[at + i * a.o_lds] = ret[i];
         }
 }
 
-// WIDTH trajectories side by side in a wave (1: a wave along time; lane = time group * WIDTH + trajectory).  A workgroup of THREADS walks steps [t0, t1) of its trajectories from the end
-// in tiles; `behind`: the advantage at t1.  WRITE: outputs; otherwise what the steps make of the advantage behind them is returned by
-// the threads of time group 0 of wave 0.
-template <typename T, int THREADS, int WIDTH, bool DENSE, bool WRITE>
+// WIDTH trajectories side by side in a wave (1: a wave along time; lane = time group * WIDTH + trajectory).  A workgroup of THREADS walks steps
+// [t0, t1) of its trajectories from the end in tiles that begin at t0 + n tiles, so that only the last one has steps missing, behind
+// the trajectory's end; `behind`: the advantage at t1, 0 unless t1 - t0 is whole tiles.  WRITE: outputs; otherwise what the steps make of the
+// advantage behind them is returned by the threads of time group 0 of wave 0.
+template <typename T, int THREADS, int WIDTH, bool DENSE, bool DONES, bool WRITE>
 __device__ Run walk(const GaeArgs &a, int64_t b, int64_t t0, int64_t t1, int64_t len, int64_t last, double behind)
 {
     constexpr int kWaves = THREADS / 64, kGroups = 64 / WIDTH, kTile = kWaves * kGroups * kSteps;
     __shared__ Run waves[kWaves][WIDTH];
     const int lane = threadIdx.x & 63, wave = threadIdx.x % THREADS >> 6, group = lane / WIDTH, col = lane % WIDTH;
-    const int64_t hi_all = t1 < last ? t1 : last;          // the longest of the trajectories side by side
-    const int64_t end = t1 < len ? t1 : len;
+    const int64_t all_steps = (t1 < last ? t1 : last) - t0;            // of the longest of the trajectories side by side
+    const int64_t top = t1 < len ? t1 : len;
     Run all{1.0, 0.0};
-    for (int64_t hi = hi_all; hi > t0; hi -= kTile) {
-        const int64_t base = hi - kTile + (int64_t)(wave * kGroups + group) * kSteps;       // may begin before t0
-        const int64_t top = hi < end ? hi : end;
-        const Steps s = load_steps<T, DENSE>(a, b, base, t0, top, len);
-        Run scan{1.0, 0.0};
-        if (__any(s.first < s.end)) scan = fold(a, s);                                // this thread's steps and all behind them in the wave
+    for (int64_t lo = t0 + (all_steps - 1) / kTile * kTile; all_steps > 0 && lo >= t0; lo -= kTile) {
+        const int64_t base = lo + (wave * kGroups + group) * kSteps;
+        const Steps s = load_steps<T, DENSE, DONES>(a, b, base, top, len);
+        Run scan = fold<DONES>(a, s);                                  // this thread's steps and all behind them in the wave
 #pragma unroll
         for (int o = WIDTH; o < 64; o <<= 1) {
             const Run r = run_down(scan, o);
@@ -187,7 +211,7 @@ __device__ Run walk(const GaeArgs &a, int64_t b, int64_t t0, int64_t t1, int64_t
         }
         if (WRITE) {
             const Run r = run_join(later, rest);
-            if (s.first < s.end) store_steps<DENSE>(a, b, s, base, __builtin_fma(r.p, behind, r.q));
+            if (s.end > 0) store_steps<DENSE, DONES>(a, b, s, base, __builtin_fma(r.p, behind, r.q));
             behind = __builtin_fma(tile.p, behind, tile.q);
         }
         all = run_join(tile, all);
@@ -217,7 +241,7 @@ __device__ __forceinline__ double behind_chunk(const GaeArgs &a, int64_t b, int 
 
 // MODE 0: whole trajectories.  Few long ones are cut into chunks: 1 folds each by itself, 2 takes the advantage behind a chunk from the runs of
 // the later ones and writes.
-template <typename T, int THREADS, bool DENSE, int MODE>
+template <typename T, int THREADS, bool DENSE, bool DONES, int MODE>
 __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS > 64 ? 4 : 2) gae_row_kernel(const GaeArgs a)
 {
     constexpr int kRows = THREADS < 256 ? 256 / THREADS : 1;
@@ -229,17 +253,17 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS > 64 ? 
         const int i = MODE == 0 ? 0 : (int)(u - b * a.chunks);
         const int64_t t0 = i * a.chunk, t1 = MODE == 0 ? a.S : t0 + a.chunk, len = length_of(a, b);
         if (MODE == 1) {
-            const Run r = walk<T, THREADS, 1, DENSE, false>(a, b, t0, t1, len, len, 0.0);
+            const Run r = walk<T, THREADS, 1, DENSE, DONES, false>(a, b, t0, t1, len, len, 0.0);
             if (threadIdx.x % THREADS == 0) a.runs[u] = make_double2(r.p, r.q);
         } else {
-            walk<T, THREADS, 1, DENSE, true>(a, b, t0, t1, len, len, MODE == 2 ? behind_chunk(a, b, i) : 0.0);
+            walk<T, THREADS, 1, DENSE, DONES, true>(a, b, t0, t1, len, len, MODE == 2 ? behind_chunk(a, b, i) : 0.0);
         }
     }
 }
 
 // Trajectories side by side in memory, steps one after the other: sixteen trajectories a workgroup, 64 bytes of each step.
 constexpr int kWidth = 16, kSideThreads = 1024;
-template <typename T, int MODE>
+template <typename T, bool DONES, int MODE>
 __global__ void __launch_bounds__(kSideThreads) gae_side_kernel(const GaeArgs a)
 {
     const int64_t sets = (a.B + kWidth - 1) / kWidth, units = sets * a.chunks;
@@ -256,7 +280,7 @@ __global__ void __launch_bounds__(kSideThreads) gae_side_kernel(const GaeArgs a)
         }
         const int64_t t0 = i * a.chunk, t1 = MODE == 0 ? a.S : t0 + a.chunk;
         if (MODE == 1) {
-            const Run r = walk<T, kSideThreads, kWidth, false, false>(a, b, t0, t1, len, last, 0.0);
+            const Run r = walk<T, kSideThreads, kWidth, false, DONES, false>(a, b, t0, t1, len, last, 0.0);
             if (threadIdx.x < kWidth && b < a.B) a.runs[b * a.chunks + i] = make_double2(r.p, r.q);
         } else {
             double behind = 0.0;
@@ -265,7 +289,7 @@ __global__ void __launch_bounds__(kSideThreads) gae_side_kernel(const GaeArgs a)
                     const double2 x = a.runs[b * a.chunks + j];
                     behind = __builtin_fma(x.x, behind, x.y);
                 }
-            walk<T, kSideThreads, kWidth, false, true>(a, b, t0, t1, len, last, behind);
+            walk<T, kSideThreads, kWidth, false, DONES, true>(a, b, t0, t1, len, last, behind);
         }
     }
 }
@@ -273,56 +297,60 @@ __global__ void __launch_bounds__(kSideThreads) gae_side_kernel(const GaeArgs a)
 constexpr int64_t kMostBlocks = 1 << 20;
 unsigned blocks_for(int64_t n) { return (unsigned)(n < kMostBlocks ? n : kMostBlocks); }
 
-template <typename T, int THREADS, bool DENSE>
+template <typename T, int THREADS, bool DENSE, bool DONES>
 void launch_row(const GaeArgs &a, hipStream_t s)
 {
     constexpr int kBlock = THREADS < 256 ? 256 : THREADS, kRows = kBlock / THREADS;
     const dim3 grid(blocks_for((a.B * a.chunks + kRows - 1) / kRows));
     if (a.chunks == 1) {
-        hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, 0>), grid, dim3(kBlock), 0, s, a);
+        hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, DONES, 0>), grid, dim3(kBlock), 0, s, a);
     } else {
-        hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, 1>), grid, dim3(kBlock), 0, s, a);
-        hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, 2>), grid, dim3(kBlock), 0, s, a);
+        hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, DONES, 1>), grid, dim3(kBlock), 0, s, a);
+        hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, DONES, 2>), grid, dim3(kBlock), 0, s, a);
     }
 }
-template <typename T, int THREADS>
-void launch_row_of(const GaeArgs &a, hipStream_t s)
+template <typename T, bool DONES>
+void launch_side(const GaeArgs &a, hipStream_t s)
 {
-    const bool dense = a.r_lds == 1 && a.v_lds == 1 && (!a.dones || a.d_lds == 1) && a.o_lds == 1;
-    if (dense) launch_row<T, THREADS, true>(a, s);
-    else launch_row<T, THREADS, false>(a, s);
+    const dim3 grid(blocks_for((a.B + kWidth - 1) / kWidth * a.chunks));
+    if (a.chunks == 1) {
+        hipLaunchKernelGGL((gae_side_kernel<T, DONES, 0>), grid, dim3(kSideThreads), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((gae_side_kernel<T, DONES, 1>), grid, dim3(kSideThreads), 0, s, a);
+        hipLaunchKernelGGL((gae_side_kernel<T, DONES, 2>), grid, dim3(kSideThreads), 0, s, a);
+    }
 }
-
+template <typename T, bool DONES>
+void launch_of(const GaeArgs &a, hipStream_t s)
+{
+    if (a.layout == kGaeSide) launch_side<T, DONES>(a, s);
+    else if (a.layout == kGaeStrided) launch_row<T, 256, false, DONES>(a, s);
+    else if (a.threads == 64) launch_row<T, 64, true, DONES>(a, s);
+    else if (a.threads == 256) launch_row<T, 256, true, DONES>(a, s);
+    else launch_row<T, 512, true, DONES>(a, s);
+}
 template <typename T>
 hipError_t launch_typed(const GaeArgs &a, hipStream_t s)
 {
-    if (a.side) {
-        const dim3 grid(blocks_for((a.B + kWidth - 1) / kWidth * a.chunks));
-        if (a.chunks == 1) {
-            hipLaunchKernelGGL((gae_side_kernel<T, 0>), grid, dim3(kSideThreads), 0, s, a);
-        } else {
-            hipLaunchKernelGGL((gae_side_kernel<T, 1>), grid, dim3(kSideThreads), 0, s, a);
-            hipLaunchKernelGGL((gae_side_kernel<T, 2>), grid, dim3(kSideThreads), 0, s, a);
-        }
-    } else if (a.threads == 64) {
-        launch_row_of<T, 64>(a, s);
-    } else if (a.threads == 256) {
-        launch_row_of<T, 256>(a, s);
-    } else {
-        launch_row_of<T, 512>(a, s);
-    }
+    if (a.dones) launch_of<T, true>(a, s);
+    else launch_of<T, false>(a, s);
     return hipGetLastError();
 }
 
 }  // namespace
 
-GaePlan plan_gae(int64_t B, int64_t S, bool side)
+GaePlan plan_gae(int64_t B, int64_t S, int layout)
 {
     GaePlan p;
-    // chunks of whole tiles, until there are two workgroups for every compute unit
-    p.threads = side ? kSideThreads : S <= 512 ? 64 : S <= 2048 || B * ((S + 4095) / 4096) < 256 ? 256 : 512;
-    const int64_t tile = side ? kSideThreads / kWidth * kSteps : (int64_t)p.threads * kSteps;
-    const int64_t tiles = (S + tile - 1) / tile, units = side ? (B + kWidth - 1) / kWidth : B;
+    // Dense rows: a wave up to 512 steps, four to 2048, eight beyond so that two rows share a compute unit (512 x up to 8192 16 us; sixteen
+    // waves, one row, 18).  Few long rows: chunks of four waves' tiles (3 x 200003 12 us; of sixteen waves' 16), until there are two workgroups
+    // for every compute unit.
+    p.threads = layout == kGaeSide ? kSideThreads
+                : layout == kGaeStrided ? 256
+                : S <= 64 * kSteps ? 64
+                : S <= 256 * kSteps || B * ((S + 4095) / 4096) < 256 ? 256 : 512;
+    const int64_t tile = layout == kGaeSide ? kSideThreads / kWidth * kSteps : (int64_t)p.threads * kSteps;
+    const int64_t tiles = (S + tile - 1) / tile, units = layout == kGaeSide ? (B + kWidth - 1) / kWidth : B;
     const int64_t want = units > 0 ? (512 + units - 1) / units : 1;
     int64_t n = want < tiles ? want : tiles;
     if (n < 1) n = 1;

@@ -53,20 +53,21 @@ struct GaeArgs {
     int64_t r_ldb, r_lds, v_ldb, v_lds, d_ldb, d_lds, o_ldb, o_lds;
     const float *bootstrap;
     const int *lengths;
-    double gamma, gamma_lambda;
+    double gamma, gamma_lambda, factor_eight;      // gamma, gamma lambda, its eighth power
     float *adv, *ret;
     double2 *runs;                 // [B][chunks] what a chunk makes of the advantage behind it: factor, summand
     int64_t chunk;                 // steps of a chunk (S rounded up: one chunk)
     int chunks;
     int threads;                   // of a trajectory
-    bool side;                     // steps of trajectories side by side
+    int layout;
 };
-// side: the steps of neighbouring trajectories are neighbours in memory.
+// How trajectories lie in memory: the steps of each one run of items, the same step of all, or neither.
+constexpr int kGaeDense = 0, kGaeSide = 1, kGaeStrided = 2;
 struct GaePlan {
     int threads, chunks;
     int64_t chunk, bytes;
 };
-GaePlan plan_gae(int64_t B, int64_t S, bool side);
+GaePlan plan_gae(int64_t B, int64_t S, int layout);
 hipError_t launch_gae(const GaeArgs &a, int type, hipStream_t s);
 
 int grad_parts(const int64_t *numels, const int32_t *types, int n);     // partial sums a norm needs room for

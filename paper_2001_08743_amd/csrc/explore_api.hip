@@ -154,9 +154,13 @@ int32_t cham_policy_loss(const void *logits, int32_t type, int64_t R, int32_t G,
 int64_t cham_gae_workspace_bytes(int64_t B, int64_t S)
 {
     if (B < 0 || S < 0 || S > 0x7fffffff || (S > 0 && B > kMostItems / S)) return CHAM_E_BAD_DIM;
-    // the larger one: the query does not ask for the layout
-    const int64_t row = plan_gae(B, S, false).bytes, side = plan_gae(B, S, true).bytes;
-    return row > side ? row : side;
+    // the largest one: the query does not ask for the layout
+    int64_t most = 0;
+    for (int layout = kGaeDense; layout <= kGaeStrided; ++layout) {
+        const int64_t n = plan_gae(B, S, layout).bytes;
+        most = n > most ? n : most;
+    }
+    return most;
 }
 
 int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_t r_ldb, int64_t r_lds,
@@ -186,9 +190,10 @@ int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_
         !aligned(advantages, 4) || !aligned(returns, 4))
         return CHAM_E_BAD_DIM;
     if (!workspace_ok(workspace, workspace_bytes, need)) return CHAM_E_WORKSPACE;
-    // trajectories side by side: rewards, values and outputs of a step stand closer together than the steps of a trajectory
-    const bool side = B >= 8 && r_ldb < r_lds && v_ldb < v_lds && o_ldb < o_lds;
-    const GaePlan p = plan_gae(B, S, side);
+    // side by side: of rewards, values and outputs the same step of all trajectories stands closer together than the steps of one
+    const bool dense = r_lds == 1 && v_lds == 1 && (!dones || d_lds == 1) && o_lds == 1;
+    const int layout = B >= 8 && r_ldb < r_lds && v_ldb < v_lds && o_ldb < o_lds ? kGaeSide : dense ? kGaeDense : kGaeStrided;
+    const GaePlan p = plan_gae(B, S, layout);
     GaeArgs a{};
     a.B = B;
     a.S = S;
@@ -206,14 +211,16 @@ int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_
     a.bootstrap = bootstrap;
     a.lengths = lengths;
     a.gamma = gamma;
-    a.gamma_lambda = gamma * lambda;
+    const double gl = gamma * lambda, gl2 = gl * gl, gl4 = gl2 * gl2;
+    a.gamma_lambda = gl;
+    a.factor_eight = gl4 * gl4;
     a.adv = advantages;
     a.ret = returns;
     a.runs = static_cast<double2 *>(workspace);
     a.chunk = p.chunk;
     a.chunks = p.chunks;
     a.threads = p.threads;
-    a.side = side;
+    a.layout = layout;
     const hipError_t h = launch_gae(a, type, reinterpret_cast<hipStream_t>(stream));
     return h == hipSuccess ? CHAM_OK : hip_fail(h);
 }
