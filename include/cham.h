@@ -418,8 +418,9 @@ typedef struct cham_policy_coef {
  *   logp, entropy DEVICE float [R], either may be NULL
  *   grad_logits DEVICE, of the logits' type, at strides gld_r, gld_g: the gradient of the total, every item written (zeros for
  *           what is left out; other memory between strides is left as it was).  NULL: forward only.  It may be the
- *           logits themselves (same pointer and strides: in place); any other overlap is refused
+ *           logits themselves (same pointer and strides: in place); otherwise their ranges of addresses must not cross
  *   grad_values DEVICE float [R] or NULL
+ * No other output shares memory with an input or another output.
  * The gradient of a minimum or maximum is that of the unclipped side where both are equal.  A term whose coefficient is
  * 0 adds nothing to the total or the gradients, whatever its value.  Exponentials are taken in fp32; differences, products
  * and sums per decision and over decisions in double.
@@ -439,7 +440,8 @@ int64_t cham_gae_workspace_bytes(int64_t B, int64_t S);
 /*
  * Advantages (generalised advantage estimation) and returns of B trajectories of up to S steps:
  *   delta_t = r_t + gamma n_t V_{t+1} - V_t,  A_t = delta_t + gamma lambda n_t A_{t+1},  ret_t = A_t + V_t,
- * n_t = 0 where done_t is set and 1 elsewhere, V behind the last step = bootstrap, A behind it = 0.
+ * n_t = 0 where done_t is set and 1 elsewhere, V behind the last step = bootstrap, A behind it = 0.  A step with done_t set
+ * takes nothing from behind it, not even a NaN; elsewhere what is no number goes to all earlier steps of its episode.
  *   rewards, values DEVICE of `type` (f32, bf16, f16): step s of trajectory b at [b*ld_b + s*ld_s], any strides >= 0
  *   dones     DEVICE uint8, same addressing, or NULL (no episode ends inside)
  *   bootstrap DEVICE float [B] or NULL (zeros): value of the state behind the last step
@@ -472,8 +474,8 @@ int64_t cham_grad_workspace_bytes(const int64_t *numels, const int32_t *types, i
  * cham_clip_grads then scales every gradient by max_norm / (norm + 1e-6) unless norm + 1e-6 <= max_norm; gradients are
  * multiplied in fp32 and rounded once.  A NaN norm makes every gradient NaN, an infinite one makes finite gradients 0.
  *   outs   HOST array of n DEVICE pointers: where the clipped gradients go (an unclipped copy where nothing is clipped);
- *          NULL: in place (not written at all where nothing is clipped).  outs[i] may be grads[i]; other overlaps are the
- *          caller's to avoid
+ *          NULL: in place (not written at all where nothing is clipped).  outs[i] may be grads[i]; otherwise no two tensors
+ *          of the call share memory
  *   flags  CHAM_F_NORM_GIVEN: *norm is read instead of computed (the norm over several processes' parts, say)
  * n = 0 gives the norm 0.  Results do not depend on the order in which workgroups run.
  * Errors: CHAM_E_NULL, CHAM_E_BAD_DIM (n < 0, a negative or too large count (2^40 in all), misaligned pointers),

@@ -751,6 +751,9 @@ class GradList:
             codes.append(_type_of(t, _FLOAT_TYPES, f"tensor {i}"))
         self.ptrs = (C.c_void_p * max(n, 1))(*[t.data_ptr() for t in self.tensors])
         self.numels = (C.c_int64 * max(n, 1))(*[t.numel() for t in self.tensors])
+        filled = [p for p, m in zip(self.ptrs, self.numels) if m > 0]
+        if len(set(filled)) != len(filled):
+            raise ChamError("a tensor stands twice in the list")
         self.types = (C.c_int32 * max(n, 1))(*codes)
         self.sizes = bytes(self.numels) + bytes(self.types)
         self.workspace_bytes = _check(load().cham_grad_workspace_bytes(self.numels, self.types, n))

@@ -18,7 +18,14 @@ constexpr int kSteps = 8;                 // consecutive steps of a thread
 struct Run {
     double p, q;                          // factor and summand
 };
-__device__ __forceinline__ Run run_join(const Run &first, const Run &later) { return {first.p * later.p, __builtin_fma(first.p, later.q, first.q)}; }
+// q + p x.  CUT (where episodes end inside): q alone where p is 0, so that an episode takes nothing from the next one, not even a NaN; a factor is
+// then 0 by an episode's end (or gamma lambda = 0), never by underflow.
+template <bool CUT>
+__device__ __forceinline__ double apply(double p, double x, double q) { return CUT && p == 0.0 ? q : __builtin_fma(p, x, q); }
+template <bool CUT>
+__device__ __forceinline__ double factor_join(double a, double b) { return CUT ? a == 0.0 || b == 0.0 ? 0.0 : fmax(a * b, 1e-300) : a * b; }
+template <bool CUT>
+__device__ __forceinline__ Run run_join(const Run &first, const Run &later) { return {factor_join<CUT>(first.p, later.p), apply<CUT>(first.p, later.q, first.q)}; }
 __device__ __forceinline__ Run run_down(const Run &r, int by) { return {__shfl_down(r.p, by), __shfl_down(r.q, by)}; }
 
 __device__ __forceinline__ int64_t length_of(const GaeArgs &a, int64_t b)
@@ -130,8 +137,8 @@ __device__ __forceinline__ Run fold(const GaeArgs &a, const Steps &s)
 #pragma unroll
     for (int i = kSteps - 2; i >= 0; --i) {
         const double c = factor_of<DONES>(a, s, i);
-        if (DONES) r.p *= c;
-        r.q = __builtin_fma(c, r.q, s.d[i]);
+        if (DONES) r.p = factor_join<true>(r.p, c);
+        r.q = apply<DONES>(c, r.q, s.d[i]);
     }
     return r;
 }
@@ -141,7 +148,7 @@ __device__ __forceinline__ void store_steps(const GaeArgs &a, int64_t b, const S
     float adv[kSteps], ret[kSteps];
 #pragma unroll
     for (int i = kSteps - 1; i >= 0; --i) {
-        behind = __builtin_fma(factor_of<DONES>(a, s, i), behind, s.d[i]);
+        behind = apply<DONES>(factor_of<DONES>(a, s, i), behind, s.d[i]);
         adv[i] = (float)behind;
         ret[i] = (float)(behind + (double)s.v[i]);
     }
@@ -171,7 +178,40 @@ __device__ __forceinline__ void store_steps(const GaeArgs &a, int64_t b, const S
         }
 }
 
-// WIDTH trajectories side by side in a wave (1: a wave along time; lane = time group * WIDTH + trajectory).  A workgroup of THREADS walks steps
+// Runs of a workgroup's threads joined: `later`: those of the threads behind this one (of the same trajectory), `all`: of all.  WIDTH
+// trajectories side by side in a wave, lane = time group * WIDTH + trajectory; waves in order of time.
+template <int THREADS, int WIDTH, bool CUT>
+__device__ __forceinline__ void join_block(const Run &own, Run &later, Run &all)
+{
+    constexpr int kWaves = THREADS / 64, kGroups = 64 / WIDTH;
+    __shared__ Run waves[kWaves][WIDTH];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x % THREADS >> 6, group = lane / WIDTH, col = lane % WIDTH;
+    Run scan = own;                                                    // this thread's and all behind it in the wave
+#pragma unroll
+    for (int o = WIDTH; o < 64; o <<= 1) {
+        const Run r = run_down(scan, o);
+        if (lane + o < 64) scan = run_join<CUT>(scan, r);
+    }
+    later = run_down(scan, WIDTH & 63);
+    if (group == kGroups - 1) later = {1.0, 0.0};
+    if (kWaves == 1) {
+        all = {__shfl(scan.p, col), __shfl(scan.q, col)};
+        return;
+    }
+    if (group == 0) waves[wave][col] = scan;
+    __syncthreads();
+    Run rest{1.0, 0.0};
+    all = {1.0, 0.0};
+#pragma unroll 2
+    for (int w = kWaves - 1; w >= 0; --w) {
+        if (w == wave) rest = all;
+        all = run_join<CUT>(waves[w][col], all);
+    }
+    later = run_join<CUT>(later, rest);
+    __syncthreads();
+}
+
+// WIDTH trajectories side by side in a wave (1: a wave along time).  A workgroup of THREADS walks steps
 // [t0, t1) of its trajectories from the end in tiles that begin at t0 + n tiles, so that only the last one has steps missing, behind
 // the trajectory's end; `behind`: the advantage at t1, 0 unless t1 - t0 is whole tiles.  WRITE: outputs; otherwise what the steps make of the
 // advantage behind them is returned by the threads of time group 0 of wave 0.
@@ -179,64 +219,40 @@ template <typename T, int THREADS, int WIDTH, bool DENSE, bool DONES, bool WRITE
 __device__ Run walk(const GaeArgs &a, int64_t b, int64_t t0, int64_t t1, int64_t len, int64_t last, double behind)
 {
     constexpr int kWaves = THREADS / 64, kGroups = 64 / WIDTH, kTile = kWaves * kGroups * kSteps;
-    __shared__ Run waves[kWaves][WIDTH];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x % THREADS >> 6, group = lane / WIDTH, col = lane % WIDTH;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x % THREADS >> 6, group = lane / WIDTH;
     const int64_t all_steps = (t1 < last ? t1 : last) - t0;            // of the longest of the trajectories side by side
     const int64_t top = t1 < len ? t1 : len;
     Run all{1.0, 0.0};
     for (int64_t lo = t0 + (all_steps - 1) / kTile * kTile; all_steps > 0 && lo >= t0; lo -= kTile) {
         const int64_t base = lo + (wave * kGroups + group) * kSteps;
         const Steps s = load_steps<T, DENSE, DONES>(a, b, base, top, len);
-        Run scan = fold<DONES>(a, s);                                  // this thread's steps and all behind them in the wave
-#pragma unroll
-        for (int o = WIDTH; o < 64; o <<= 1) {
-            const Run r = run_down(scan, o);
-            if (lane + o < 64) scan = run_join(scan, r);
-        }
-        Run later = run_down(scan, WIDTH & 63);
-        if (group == kGroups - 1) later = {1.0, 0.0};
-        Run tile = scan, rest{1.0, 0.0};
-        if (kWaves > 1) {
-            if (group == 0) waves[wave][col] = scan;
-            __syncthreads();
-            tile = {1.0, 0.0};
-#pragma unroll 2
-            for (int w = kWaves - 1; w >= 0; --w) {
-                if (w == wave) rest = tile;
-                tile = run_join(waves[w][col], tile);
-            }
-            __syncthreads();
-        } else {
-            tile = {__shfl(scan.p, col), __shfl(scan.q, col)};
-        }
+        Run later, tile;
+        join_block<THREADS, WIDTH, DONES>(fold<DONES>(a, s), later, tile);
         if (WRITE) {
-            const Run r = run_join(later, rest);
-            if (s.end > 0) store_steps<DENSE, DONES>(a, b, s, base, __builtin_fma(r.p, behind, r.q));
-            behind = __builtin_fma(tile.p, behind, tile.q);
+            if (s.end > 0) store_steps<DENSE, DONES>(a, b, s, base, apply<DONES>(later.p, behind, later.q));
+            behind = apply<DONES>(tile.p, behind, tile.q);
         }
-        all = run_join(tile, all);
+        all = run_join<DONES>(tile, all);
     }
     return all;
 }
 
-// The advantage behind chunk i of a trajectory, from the runs of the later ones: a lane joins some consecutive ones, then the lanes.
+// The advantage behind chunk i of a trajectory, from the runs of the later ones: a thread joins some consecutive ones, then the threads.
+template <int THREADS, int WIDTH, bool CUT>
 __device__ __forceinline__ double behind_chunk(const GaeArgs &a, int64_t b, int i)
 {
-    const int lane = threadIdx.x & 63, n = a.chunks - 1 - i, per = (n + 63) / 64;
-    Run r{1.0, 0.0};
+    constexpr int kShares = THREADS / WIDTH;
+    const int share = threadIdx.x % THREADS / WIDTH, n = a.chunks - 1 - i, per = (n + kShares - 1) / kShares;
+    Run own{1.0, 0.0}, later, all;
     for (int k = per - 1; k >= 0; --k) {
-        const int j = i + 1 + lane * per + k;
+        const int j = i + 1 + share * per + k;
         if (j < a.chunks && b < a.B) {
             const double2 x = a.runs[b * a.chunks + j];
-            r = run_join({x.x, x.y}, r);
+            own = run_join<CUT>({x.x, x.y}, own);
         }
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const Run x = run_down(r, o);
-        if (lane + o < 64) r = run_join(r, x);
-    }
-    return __shfl(r.q, 0);
+    join_block<THREADS, WIDTH, CUT>(own, later, all);
+    return all.q;
 }
 
 // MODE 0: whole trajectories.  Few long ones are cut into chunks: 1 folds each by itself, 2 takes the advantage behind a chunk from the runs of
@@ -256,7 +272,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS > 64 ? 
             const Run r = walk<T, THREADS, 1, DENSE, DONES, false>(a, b, t0, t1, len, len, 0.0);
             if (threadIdx.x % THREADS == 0) a.runs[u] = make_double2(r.p, r.q);
         } else {
-            walk<T, THREADS, 1, DENSE, DONES, true>(a, b, t0, t1, len, len, MODE == 2 ? behind_chunk(a, b, i) : 0.0);
+            walk<T, THREADS, 1, DENSE, DONES, true>(a, b, t0, t1, len, len, MODE == 2 ? behind_chunk<THREADS, 1, DONES>(a, b, i) : 0.0);
         }
     }
 }
@@ -283,12 +299,7 @@ __global__ void __launch_bounds__(kSideThreads) gae_side_kernel(const GaeArgs a)
             const Run r = walk<T, kSideThreads, kWidth, false, DONES, false>(a, b, t0, t1, len, last, 0.0);
             if (threadIdx.x < kWidth && b < a.B) a.runs[b * a.chunks + i] = make_double2(r.p, r.q);
         } else {
-            double behind = 0.0;
-            if (MODE == 2 && b < a.B)
-                for (int j = a.chunks - 1; j > i; --j) {
-                    const double2 x = a.runs[b * a.chunks + j];
-                    behind = __builtin_fma(x.x, behind, x.y);
-                }
+            const double behind = MODE == 2 ? behind_chunk<kSideThreads, kWidth, DONES>(a, b, i) : 0.0;
             walk<T, kSideThreads, kWidth, false, DONES, true>(a, b, t0, t1, len, last, behind);
         }
     }

@@ -280,7 +280,7 @@ def test_binding_refuses():
            lambda: binding.cham_policy_loss(x.expand(4, 3)[:1].expand(4, 3), a, z, z),
            lambda: binding.cham_gae(x, x.bfloat16(), 0.9, 0.9), lambda: binding.cham_gae(x, x, 1.9, 0.9), lambda: binding.cham_gae(x, x, 0.9, 0.9, lengths=a),
            lambda: binding.cham_gae(x, x[:, :2], 0.9, 0.9), lambda: binding.cham_clip_grads([x.t()], 1.0), lambda: binding.cham_clip_grads([x, x.cpu()], 1.0),
-           lambda: binding.cham_clip_grads([x], -1.0), lambda: binding.cham_clip_grads([x], 1.0, out=[x, x]), lambda: binding.cham_clip_grads([x], 1.0, out=[x.half()]),
+           lambda: binding.cham_clip_grads([x], -1.0), lambda: binding.cham_clip_grads([x, z, x], 1.0), lambda: binding.cham_clip_grads([x], 1.0, out=[x, x]), lambda: binding.cham_clip_grads([x], 1.0, out=[x.half()]),
            lambda: binding.cham_clip_grads([x], 1.0, norm_given=True), lambda: binding.cham_grad_norm([a])]
     for f in bad:
         with pytest.raises(binding.ChamError):
@@ -346,6 +346,38 @@ def test_gae_steps_behind_a_length_are_not_read_and_lengths_are_held():
     only = binding.cham_gae(r.to(DEV), v.to(DEV), 0.9, 0.9, bootstrap=i["bootstrap"].to(DEV), lengths=i["lengths"].to(DEV),
                             out=dict(advantages=torch.zeros(6, 40, device=DEV), returns=None))
     assert torch.equal(only["advantages"], got["advantages"])
+
+
+@pytest.mark.parametrize("B,S,at", [(9, 70, 33), (9, 70, 32), (2, 3000, 1999), (1, 60000, 40000)])
+def test_gae_an_episode_keeps_its_nan(B, S, at):
+    i = _gae_inputs(B, S, torch.float32, 91)
+    i["dones"][:] = 0
+    i["dones"][:, at] = 1                                 # the last step of the first episode
+    for place in (lambda t: t.to(DEV), lambda t: t.to(DEV).t().contiguous().t()):
+        run = lambda: binding.cham_gae(place(i["rewards"]), place(i["values"]), 1.0, 1.0, dones=place(i["dones"]))["advantages"]
+        i["rewards"][:, S - 1] = 1.0
+        clean = run()
+        i["rewards"][:, S - 1] = math.nan                 # of the second
+        got = run()
+        assert torch.equal(got[:, :at + 1], clean[:, :at + 1])
+        assert torch.isnan(got[:, at + 1:]).all()
+        i["rewards"][:, S - 1] = 1.0
+    # factors that become too small for a double do not end an episode
+    v = torch.zeros(1, 20000, device=DEV)
+    r = torch.zeros(1, 20000, device=DEV)
+    r[0, -1] = math.nan
+    assert torch.isnan(binding.cham_gae(r, v, 0.5, 0.5)["advantages"]).all()
+
+
+def test_gae_side_by_side_in_many_chunks():
+    B, S = 20, 40001
+    i = _gae_inputs(B, S, torch.float32, 77)
+    i["lengths"][:3] = torch.tensor([S, 1, 512])
+    adv, ret, there = ref.gae(i["rewards"], i["values"], 1.0, 0.999, i["dones"], i["bootstrap"], i["lengths"])
+    side = lambda t: t.to(DEV).t().contiguous().t()
+    got = binding.cham_gae(side(i["rewards"]), side(i["values"]), 1.0, 0.999, dones=side(i["dones"]), bootstrap=i["bootstrap"].to(DEV), lengths=i["lengths"].to(DEV))
+    assert got["advantages"].stride() == (1, B)
+    _check_gae(got, (adv, ret), there)
 
 
 def test_gae_shared_rewards_and_no_trajectories():
