@@ -579,39 +579,40 @@ def _type_of(t, types, what: str) -> int:
     return code
 
 
-def _stream_of(device):
-    """Current stream of a device that has to be the current one (kernels are launched there)."""
+def _stream_of(t, what: str):
+    """(device, its index, its current stream) of a tensor on the current device (kernels are launched there)."""
     torch = _torch()
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ChamError(f"tensors on {device}, current device cuda:{torch.cuda.current_device()}")
-    return torch._C._cuda_getCurrentRawStream(device.index)
+    index = t.get_device()
+    if index < 0 or index != torch._C._cuda_getDevice():
+        raise ChamError(f"{what}: on {t.device}, current device cuda:{torch.cuda.current_device()}")
+    return t.device, index, torch._C._cuda_getCurrentRawStream(index)
 
 
-def _addr(t, device, what: str, dtype, shape):
-    """Address of an optional tensor that has to lie on `device`, dense, with this type and shape."""
+def _addr(t, index: int, what: str, dtype, shape):
+    """Address of an optional tensor that has to lie on the device with this index, dense, with this type and shape."""
     if t is None:
         return None
-    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+    if t.dtype is dtype and t.get_device() == index and t.shape == shape and t.is_contiguous():
         return t.data_ptr()
-    raise ChamError(f"{what}: need a dense {dtype} tensor of shape {tuple(shape)} on {device}, "
+    raise ChamError(f"{what}: need a dense {dtype} tensor of shape {tuple(shape)} on cuda:{index}, "
                     f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
 
 
-def _scratch(workspace, device, nbytes, *sizes):
+def _scratch(workspace, device, index: int, nbytes, *sizes):
     """The caller's workspace, or one of nbytes(*sizes) bytes; and its address."""
     if workspace is None:
         workspace = _torch().empty(max(nbytes(*sizes), 256), dtype=_torch().uint8, device=device)
-    elif workspace.device != device or not workspace.is_contiguous() or workspace.element_size() != 1:
+    elif workspace.get_device() != index or not workspace.is_contiguous() or workspace.element_size() != 1:
         raise ChamError(f"workspace: need dense bytes on {device}, got {workspace.dtype} strides {workspace.stride()} on {workspace.device}")
     return workspace, workspace.data_ptr()
 
 
 def _heads(logits, what: str):
     """(R, G, V, ld_r, ld_g) of logits [R, V] or [R, G, V] whose choices are consecutive."""
-    if logits.dim() not in (2, 3) or (logits.shape[-1] > 1 and logits.stride(-1) != 1):
-        raise ChamError(f"{what}: need [R, V] or [R, G, V] with consecutive choices, got {tuple(logits.shape)} strides {logits.stride()}")
-    R, V = logits.shape[0], logits.shape[-1]
-    return (R, 1, V, logits.stride(0), 0) if logits.dim() == 2 else (R, logits.shape[1], V, logits.stride(0), logits.stride(1))
+    shape, stride = logits.shape, logits.stride()
+    if len(shape) not in (2, 3) or (stride[-1] != 1 and shape[-1] > 1):
+        raise ChamError(f"{what}: need [R, V] or [R, G, V] with consecutive choices, got {tuple(shape)} strides {stride}")
+    return (shape[0], 1, shape[1], stride[0], 0) if len(shape) == 2 else (*shape, stride[0], stride[1])
 
 
 def cham_policy_workspace_bytes(R: int, G: int, V: int, type: int, want_grad: bool) -> int:
@@ -622,16 +623,15 @@ def cham_policy_logp(logits, actions, first_action: int = 0, weights=None, out: 
     """Log-probability of the actions and entropy per decision.  logits [R, V] or [R, G, V] (f32, bf16, f16; choices
     consecutive), actions [R] or [R, G] (int8, int32, int64); returns a dict of float tensors logp [R], entropy [R]."""
     torch = _torch()
-    dev = logits.device
-    stream = _stream_of(dev)
+    dev, index, stream = _stream_of(logits, "logits")
     R, G, V, ld_r, ld_g = _heads(logits, "logits")
     code = _type_of(logits, _FLOAT_TYPES, "logits")
-    acts = _addr(actions, dev, "actions", actions.dtype, logits.shape[:-1])
+    acts = _addr(actions, index, "actions", actions.dtype, logits.shape[:-1])
     out = dict(out) if out is not None else dict(logp=torch.empty(R, dtype=torch.float32, device=dev), entropy=torch.empty(R, dtype=torch.float32, device=dev))
-    workspace, at = _scratch(workspace, dev, cham_policy_workspace_bytes, R, G, V, code, False)
+    workspace, at = _scratch(workspace, dev, index, cham_policy_workspace_bytes, R, G, V, code, False)
     _check(load().cham_policy_logp(logits.data_ptr(), code, R, G, V, ld_r, ld_g, acts, _type_of(actions, _ACTION_TYPES, "actions"), first_action,
-                                   _addr(weights, dev, "weights", torch.float32, (R,)), _addr(out["logp"], dev, "logp", torch.float32, (R,)),
-                                   _addr(out.get("entropy"), dev, "entropy", torch.float32, (R,)), at, workspace.numel(), stream))
+                                   _addr(weights, index, "weights", torch.float32, (R,)), _addr(out["logp"], index, "logp", torch.float32, (R,)),
+                                   _addr(out.get("entropy"), index, "entropy", torch.float32, (R,)), at, workspace.numel(), stream))
     out["workspace"] = workspace
     return out
 
@@ -643,12 +643,11 @@ def cham_policy_loss(logits, actions, old_logp, advantages, first_action: int = 
     grad_logits (like logits) and grad_values [R] (None without want_grad, or without values).  ``out`` holds the caller's
     tensors under these names; out["grad_logits"] may be the logits themselves."""
     torch = _torch()
-    dev = logits.device
-    stream = _stream_of(dev)
+    dev, index, stream = _stream_of(logits, "logits")
     R, G, V, ld_r, ld_g = _heads(logits, "logits")
     code = _type_of(logits, _FLOAT_TYPES, "logits")
     f32 = torch.float32
-    acts = _addr(actions, dev, "actions", actions.dtype, logits.shape[:-1])
+    acts = _addr(actions, index, "actions", actions.dtype, logits.shape[:-1])
     if out is None:
         rows = torch.empty((2, R), dtype=f32, device=dev)
         out = dict(terms=torch.empty(len(TERMS), dtype=f32, device=dev), logp=rows[0], entropy=rows[1],
@@ -659,7 +658,7 @@ def cham_policy_loss(logits, actions, old_logp, advantages, first_action: int = 
     grad = out.get("grad_logits") if want_grad else None
     gld_r = gld_g = 0
     if grad is not None:
-        if grad.dtype != logits.dtype or grad.shape != logits.shape or grad.device != dev:
+        if grad.dtype is not logits.dtype or grad.shape != logits.shape or grad.get_device() != index:
             raise ChamError(f"grad_logits: need {logits.dtype} {tuple(logits.shape)} on {dev}, got {grad.dtype} {tuple(grad.shape)} on {grad.device}")
         _, _, _, gld_r, gld_g = _heads(grad, "grad_logits")
     row = (R,)
@@ -669,15 +668,15 @@ def cham_policy_loss(logits, actions, old_logp, advantages, first_action: int = 
     for i, t in enumerate(rows):                        # as _addr, ten of them a call
         if t is None:
             at.append(None)
-        elif t.dtype is f32 and t.shape == row and t.device == dev and t.is_contiguous():
+        elif t.dtype is f32 and t.get_device() == index and t.shape == row and t.is_contiguous():
             at.append(t.data_ptr())
         else:
-            _addr(t, dev, _LOSS_ROWS[i], f32, row)
+            _addr(t, index, _LOSS_ROWS[i], f32, row)
     coef = _PolicyCoef(clip_low, clip_high, value_coef, entropy_coef, kl_coef, value_clip)
-    workspace, ws = _scratch(workspace, dev, cham_policy_workspace_bytes, R, G, V, code, grad is not None)
+    workspace, ws = _scratch(workspace, dev, index, cham_policy_workspace_bytes, R, G, V, code, grad is not None)
     _check(load().cham_policy_loss(
         logits.data_ptr(), code, R, G, V, ld_r, ld_g, acts, _type_of(actions, _ACTION_TYPES, "actions"), first_action, *at[:7], coef,
-        _addr(out["terms"], dev, "terms", f32, (len(TERMS),)), at[7], at[8], None if grad is None else grad.data_ptr(), gld_r, gld_g, at[9],
+        _addr(out["terms"], index, "terms", f32, (len(TERMS),)), at[7], at[8], None if grad is None else grad.data_ptr(), gld_r, gld_g, at[9],
         ws, workspace.numel(), stream))
     out["workspace"] = workspace
     return out
@@ -686,12 +685,12 @@ def cham_policy_loss(logits, actions, old_logp, advantages, first_action: int = 
 _LOSS_ROWS = ("weights", "old_logp", "advantages", "ref_logp", "values", "old_values", "returns", "logp", "entropy", "grad_values")
 
 
-def _matrix(t, device, what: str, dtype, shape):
+def _matrix(t, index: int, what: str, dtype, shape):
     """(address, stride of trajectories, stride of steps) of an optional [B, S] tensor of any strides."""
     if t is None:
         return None, 0, 0
-    if t.device != device or t.dtype is not dtype or t.shape != shape:
-        raise ChamError(f"{what}: need {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.get_device() != index or t.dtype is not dtype or t.shape != shape:
+        raise ChamError(f"{what}: need {dtype} {tuple(shape)} on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return (t.data_ptr(), *t.stride())
 
 
@@ -705,8 +704,7 @@ def cham_gae(rewards, values, gamma: float, lam: float, dones=None, bootstrap=No
     ``out`` holds advantages and returns (float, of one layout; returns may be None); without it they are made like
     rewards, zero behind a length."""
     torch = _torch()
-    dev = rewards.device
-    stream = _stream_of(dev)
+    dev, index, stream = _stream_of(rewards, "rewards")
     if rewards.dim() != 2:
         raise ChamError(f"rewards: need [B, S], got {tuple(rewards.shape)}")
     B, S = shape = rewards.shape
@@ -719,16 +717,16 @@ def cham_gae(rewards, values, gamma: float, lam: float, dones=None, bootstrap=No
         out = dict(advantages=pair[0], returns=pair[1])
     else:
         out = dict(out)
-    r, r_b, r_s = _matrix(rewards, dev, "rewards", rewards.dtype, shape)
-    v, v_b, v_s = _matrix(values, dev, "values", rewards.dtype, shape)
-    d, d_b, d_s = _matrix(dones, dev, "dones", torch.uint8, shape)
-    adv, o_b, o_s = _matrix(out["advantages"], dev, "advantages", torch.float32, shape)
-    ret, q_b, q_s = _matrix(out.get("returns"), dev, "returns", torch.float32, shape)
+    r, r_b, r_s = _matrix(rewards, index, "rewards", rewards.dtype, shape)
+    v, v_b, v_s = _matrix(values, index, "values", rewards.dtype, shape)
+    d, d_b, d_s = _matrix(dones, index, "dones", torch.uint8, shape)
+    adv, o_b, o_s = _matrix(out["advantages"], index, "advantages", torch.float32, shape)
+    ret, q_b, q_s = _matrix(out.get("returns"), index, "returns", torch.float32, shape)
     if ret is not None and (q_b, q_s) != (o_b, o_s):
         raise ChamError("returns: need the strides of advantages")
-    workspace, at = _scratch(workspace, dev, cham_gae_workspace_bytes, B, S)
-    _check(load().cham_gae(code, B, S, r, r_b, r_s, v, v_b, v_s, d, d_b, d_s, _addr(bootstrap, dev, "bootstrap", torch.float32, (B,)),
-                           _addr(lengths, dev, "lengths", torch.int32, (B,)), gamma, lam, adv, ret, o_b, o_s,
+    workspace, at = _scratch(workspace, dev, index, cham_gae_workspace_bytes, B, S)
+    _check(load().cham_gae(code, B, S, r, r_b, r_s, v, v_b, v_s, d, d_b, d_s, _addr(bootstrap, index, "bootstrap", torch.float32, (B,)),
+                           _addr(lengths, index, "lengths", torch.int32, (B,)), gamma, lam, adv, ret, o_b, o_s,
                            at, workspace.numel(), stream))
     out["workspace"] = workspace
     return out
@@ -762,12 +760,13 @@ class GradList:
 def _grad_call(grads, norm, workspace):
     torch = _torch()
     grads = grads if isinstance(grads, GradList) else GradList(grads)
-    dev = grads.device if grads.n else torch.device("cuda", torch.cuda.current_device())
-    stream = _stream_of(dev)
     if norm is None:
-        norm = torch.empty(1, dtype=torch.float64, device=dev)
-    workspace, at = _scratch(workspace, dev, int, grads.workspace_bytes)
-    return grads, norm, _addr(norm, dev, "norm", torch.float64, (1,)), workspace, at, stream
+        norm = torch.empty(1, dtype=torch.float64, device=grads.device if grads.n else "cuda")
+    dev, index, stream = _stream_of(norm, "norm")
+    if grads.n and grads.device != dev:
+        raise ChamError(f"gradients on {grads.device}, current device {dev}")
+    workspace, at = _scratch(workspace, dev, index, int, grads.workspace_bytes)
+    return grads, norm, _addr(norm, index, "norm", torch.float64, (1,)), workspace, at, stream
 
 
 def cham_grad_workspace_bytes(grads) -> int:
