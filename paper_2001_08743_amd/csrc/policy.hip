@@ -626,8 +626,8 @@ __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs 
 
 // --- one head of more choices: a row stays in the registers of a wave or a workgroup between its sums and its gradient
 
-// Waves of a SIMD that the registers of N pieces a thread leave room for.
-constexpr int row_waves(int n) { return n >= 16 ? 4 : n >= 8 ? 5 : 6; }
+// Waves of a SIMD that n pieces a thread leave room for (in registers; beyond eight in LDS).
+constexpr int row_waves(int n) { return n > 8 ? 4 : n == 8 ? 5 : 6; }
 
 template <typename T>
 __device__ __forceinline__ uint4 masked_items()          // 16 bytes of -inf
@@ -676,13 +676,16 @@ struct RowAt {
     int head, n_vec, tail;
 };
 
-// THREADS of a row hold N x 16 bytes of it each, and its ends up to the first and from the last 16-byte boundary an item each; what is left of
-// longer rows is read once for the sums and once for the gradient.  A workgroup stays, and asks for a piece of its next row as
-// soon as it is done with that of the present one, so that loads are under way while sums are joined and gradients stored.
-template <typename T, int THREADS, int N, bool GRAD, bool ENT>
-__global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_waves(N)) policy_row_kernel(const PolicyArgs a)
+// THREADS of a row hold N x 16 bytes of it each in registers and L x 16 in LDS, and its ends up to the first and from the last 16-byte boundary
+// an item each; what is left of longer rows is read once for the sums and once for the gradient.  A workgroup stays, and asks for a
+// piece of its next row's N as soon as it is done with that of the present one, so that loads are under way while sums are joined and gradients
+// stored.
+template <typename T, int THREADS, int N, int L, bool GRAD, bool ENT>
+__global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_waves(N + L)) policy_row_kernel(const PolicyArgs a)
 {
     constexpr int kBlock = THREADS < kThreads ? kThreads : THREADS, kRows = kBlock / THREADS;
+    constexpr int kHeld = (N + L) * THREADS;             // pieces of a row that are read once
+    __shared__ uint4 stash[L > 0 ? L : 1][L > 0 ? kBlock : 1];
     __shared__ Soft lds[THREADS / 64];
     __shared__ float2 dec;
     __shared__ double sum[kRows][kPolicySums];           // of the rows of a group so far, by its first thread
@@ -725,6 +728,12 @@ __global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_w
         Soft v = soft_none();
         if (c >= 0) {
             Scale k2 = scale_of(v.m);
+            uint4 rest[L > 0 ? L : 1];
+#pragma unroll
+            for (int l = 0; l < L; ++l) {
+                rest[l] = masked_items<T>();
+                if (tid + (N + l) * THREADS < n_vec) rest[l] = body[tid + (N + l) * THREADS];
+            }
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 if (k * THREADS < n_vec) {               // of all threads
@@ -735,7 +744,15 @@ __global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_w
                 if (!GRAD) ask(r + step, next, k);
                 else keep_packed(held[k]);
             }
-            for (int i = tid + N * THREADS; i < n_vec; i += THREADS) {
+#pragma unroll
+            for (int l = 0; l < L; ++l)
+                if ((N + l) * THREADS < n_vec) {
+                    float x[T::kVec];
+                    T::unpack(rest[l], x);
+                    soft_add_all(v, k2, x);
+                    if (GRAD) stash[l][threadIdx.x] = rest[l];
+                }
+            for (int i = tid + kHeld; i < n_vec; i += THREADS) {
                 float x[T::kVec];
                 T::unpack(body[i], x);
                 soft_add_all(v, k2, x);
@@ -778,7 +795,10 @@ __global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_w
                 ask(r + step, next, k);
             }
             if (in) {
-                for (int i = tid + N * THREADS; i < n_vec; i += THREADS) write(i, body[i]);
+#pragma unroll
+                for (int l = 0; l < L; ++l)
+                    if (tid + (N + l) * THREADS < n_vec) write(tid + (N + l) * THREADS, stash[l][threadIdx.x]);
+                for (int i = tid + kHeld; i < n_vec; i += THREADS) write(i, body[i]);
                 if (end_at >= 0) to[end_at] = T::put(slope_at<ENT>(f, end[0]));
                 // the action's item once more, by the thread that has written it
                 const bool owner = c < head || c >= head + n_vec * T::kVec ? end_at == c : (c - head) / T::kVec % THREADS == tid;
@@ -951,8 +971,10 @@ constexpr int kWaveChunk = 2048;                // choices of a part that a wave
 constexpr int kJoinFew = 16;                    // decisions that one workgroup joins, a wave each
 
 // A wave or a workgroup per row, by its pieces of 16 bytes: 64 threads up to 1024 pieces (four rows a workgroup, no barrier), 256 up to
-// 4096, 512 beyond, up to sixteen pieces a thread.  us a loss, bf16, 64 / 256 threads: 6001 x 8191 42 / 49, 16384 x 4096 64 / 81; 256 / 512:
-// 8192 x 32768 (256 / 1024) 229 / 286, 4096 x 65536 249 / 236; 512 / 1024: 4096 x 65536 236 / 272, 4096 x 131072 510 / 497, fp32 1024 x 131072 255 / 244.
+// 4096, 512 to 8192, 1024 beyond, up to sixteen pieces a thread, of which eight in registers and eight in LDS (sixteen in registers: bf16 8192 x
+// 20001 146 us / 137, 4096 x 50021 186 / 178, fp32 16384 x 4000 105 / 100, and with 1024 threads they spill).  us a loss, bf16, 64 / 256 threads: 6001 x 8191
+// 42 / 49, 16384 x 4096 64 / 81; 256 / 512: 4096 x 65536 249 / 213; 512 / 1024: 4096 x 65536 213 / 237, 4096 x 131072 483 / 413 (the rest of a
+// row read twice; a copy of as many bytes 390), fp32 4096 x 50021 341 / 330, 1024 x 131072 249 / 236.
 // Fewer rows than what fills the chip take the next size, as a row is then all latency: 512 x 8192 15.0 / 11.5, 1024 x 8192
 // 17.0 / 16.6, 1024 x 4096 12.1 / 12.9; fp32 256 x 16384 (4096 pieces; 256 / 1024) 15.6 / 14.3, bf16 (2048 pieces) 12.1 / 12.5.
 // Beyond 4096 pieces log-probabilities alone take a row in parts, which a workgroup reads without holding it (bf16 4096 x 131072,
@@ -976,10 +998,11 @@ hipError_t launch_terms(const PolicyArgs &a, unsigned blocks, hipStream_t s)
 template <typename T, int THREADS, int N>
 void launch_row_of(const PolicyArgs &a, unsigned blocks, hipStream_t s)
 {
+    constexpr int kRegisters = N < 8 ? N : 8, kLds = N - kRegisters;
     const dim3 block(THREADS < kThreads ? kThreads : THREADS);
-    if (!a.grad) hipLaunchKernelGGL((policy_row_kernel<T, THREADS, (N < 8 ? N : 8), false, false>), dim3(blocks), block, 0, s, a);
-    else if (a.c_entropy != 0.0) hipLaunchKernelGGL((policy_row_kernel<T, THREADS, N, true, true>), dim3(blocks), block, 0, s, a);
-    else hipLaunchKernelGGL((policy_row_kernel<T, THREADS, N, true, false>), dim3(blocks), block, 0, s, a);
+    if (!a.grad) hipLaunchKernelGGL((policy_row_kernel<T, THREADS, kRegisters, 0, false, false>), dim3(blocks), block, 0, s, a);
+    else if (a.c_entropy != 0.0) hipLaunchKernelGGL((policy_row_kernel<T, THREADS, kRegisters, kLds, true, true>), dim3(blocks), block, 0, s, a);
+    else hipLaunchKernelGGL((policy_row_kernel<T, THREADS, kRegisters, kLds, true, false>), dim3(blocks), block, 0, s, a);
 }
 template <typename T>
 void launch_row(const PolicyArgs &a, const PolicyPlan &p, unsigned blocks, hipStream_t s)
@@ -994,7 +1017,8 @@ void launch_row(const PolicyArgs &a, const PolicyPlan &p, unsigned blocks, hipSt
     case 256 + 8: return launch_row_of<T, 256, 8>(a, blocks, s);
     case 256 + 16: return launch_row_of<T, 256, 16>(a, blocks, s);
     case 512 + 8: return launch_row_of<T, 512, 8>(a, blocks, s);
-    default: return launch_row_of<T, 512, 16>(a, blocks, s);
+    case 512 + 16: return launch_row_of<T, 512, 16>(a, blocks, s);
+    default: return launch_row_of<T, 1024, 16>(a, blocks, s);
     }
 }
 
@@ -1090,13 +1114,14 @@ PolicyPlan plan_policy(int64_t R, int G, int V, int type, bool grad)
     }
     const int vecs = V / (16 / type_bytes(type));
     if (G == 1 && (vecs <= kWideRow || (grad && R * 256 > vecs))) {
-        p.threads = vecs <= 1024 ? 64 : vecs <= kWideRow ? 256 : 512;
+        p.threads = vecs <= 1024 ? 64 : vecs <= kWideRow ? 256 : vecs <= 2 * kWideRow ? 512 : 1024;
         if (R < kFewRows && vecs > 256 && vecs <= 1024) p.threads = 256;
-        if (R <= kVeryFewRows && vecs > 2048) p.threads = 512;
+        if (R <= kVeryFewRows && vecs > 2048 && vecs <= kWideRow) p.threads = 512;
         const int n = (vecs + p.threads - 1) / p.threads;
         p.row = n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : n <= 8 ? 8 : 16;
         if (p.threads == 256 && p.row < 4) p.row = 4;
         if (p.threads == 512 && p.row < 8) p.row = 8;
+        if (p.threads == 1024) p.row = 16;
         p.bytes = (int64_t)kRowBlocks * kPolicySums * 8;
         return p;
     }

@@ -82,7 +82,7 @@ def _check_loss(got, want, G, V):
 
 SHAPES = [(1, 1, 1), (1, 1, 2), (5, 3, 3), (130, 24, 3), (1037, 5, 3), (7, 64, 2), (33, 12, 24), (3, 200, 7), (2, 300, 3), (2, 1100, 4), (2, 1025, 9), (50, 7, 40), (4, 64, 64), (9, 5, 70), (6, 90, 130), (3, 1, 255), (4, 1, 256), (2, 1, 257),
           (17, 1, 1000), (300, 1, 33), (2, 3, 5000), (70, 2, 300), (3, 1, 4097), (5, 1, 8191), (600, 1, 2049), (2, 1, 50021), (1, 1, 131072),
-          (3, 1, 140001), (1, 2, 270000)]
+          (3, 1, 140001), (1, 2, 270000), (600, 1, 33000), (270, 1, 70001), (260, 1, 140003)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=lambda t: str(t)[6:])
