@@ -133,14 +133,10 @@ __device__ __forceinline__ double factor_of(const GaeArgs &a, const Steps &s, in
 template <bool DONES>
 __device__ __forceinline__ Run fold(const GaeArgs &a, const Steps &s)
 {
-    Run r{DONES ? factor_of<DONES>(a, s, kSteps - 1) : a.factor_eight, s.d[kSteps - 1]};
+    double q = s.d[kSteps - 1];
 #pragma unroll
-    for (int i = kSteps - 2; i >= 0; --i) {
-        const double c = factor_of<DONES>(a, s, i);
-        if (DONES) r.p = factor_join<true>(r.p, c);
-        r.q = apply<DONES>(c, r.q, s.d[i]);
-    }
-    return r;
+    for (int i = kSteps - 2; i >= 0; --i) q = apply<DONES>(factor_of<DONES>(a, s, i), q, s.d[i]);
+    return {DONES && s.done != 0 ? 0.0 : a.factor_eight, q};
 }
 template <bool DENSE, bool DONES>
 __device__ __forceinline__ void store_steps(const GaeArgs &a, int64_t b, const Steps &s, int64_t base, double behind)
@@ -247,7 +243,7 @@ __device__ __forceinline__ double behind_chunk(const GaeArgs &a, int64_t b, int 
     for (int k = per - 1; k >= 0; --k) {
         const int j = i + 1 + share * per + k;
         if (j < a.chunks && b < a.B) {
-            const double2 x = a.runs[b * a.chunks + j];
+            const double2 x = a.runs[WIDTH == 1 ? b * a.chunks + j : j * a.B + b];
             own = run_join<CUT>({x.x, x.y}, own);
         }
     }
@@ -277,30 +273,32 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS, THREADS > 64 ? 
     }
 }
 
-// Trajectories side by side in memory, steps one after the other: sixteen trajectories a workgroup, 64 bytes of each step.
-constexpr int kWidth = 16, kSideThreads = 1024;
-template <typename T, bool DONES, int MODE>
+// Trajectories side by side in memory, steps one after the other: WIDTH trajectories a workgroup, whose items of a step are one run.
+// Two workgroups share a compute unit, so that one loads while the other joins (1024 threads,
+// one workgroup: 726 x 4630 fp32 45 us / 38, 64 x 65536 30 / 22).
+constexpr int kSideThreads = 512;
+template <typename T, int WIDTH, bool DONES, int MODE>
 __global__ void __launch_bounds__(kSideThreads) gae_side_kernel(const GaeArgs a)
 {
-    const int64_t sets = (a.B + kWidth - 1) / kWidth, units = sets * a.chunks;
-    const int col = threadIdx.x % kWidth;
+    const int64_t sets = (a.B + WIDTH - 1) / WIDTH, units = sets * a.chunks;
+    const int col = threadIdx.x % WIDTH;
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int64_t set = MODE == 0 ? u : u / a.chunks, b = set * kWidth + col;
+        const int64_t set = MODE == 0 ? u : u / a.chunks, b = set * WIDTH + col;
         const int i = (int)(u - set * a.chunks);
         const int64_t len = b < a.B ? length_of(a, b) : 0;              // 0: nothing of it is read or written
         int64_t last = len;                                             // the longest of those side by side
 #pragma unroll
-        for (int o = 1; o < kWidth; o <<= 1) {
+        for (int o = 1; o < WIDTH; o <<= 1) {
             const int64_t x = __shfl_xor(last, o);
             last = x > last ? x : last;
         }
         const int64_t t0 = i * a.chunk, t1 = MODE == 0 ? a.S : t0 + a.chunk;
         if (MODE == 1) {
-            const Run r = walk<T, kSideThreads, kWidth, false, DONES, false>(a, b, t0, t1, len, last, 0.0);
-            if (threadIdx.x < kWidth && b < a.B) a.runs[b * a.chunks + i] = make_double2(r.p, r.q);
+            const Run r = walk<T, kSideThreads, WIDTH, false, DONES, false>(a, b, t0, t1, len, last, 0.0);
+            if (threadIdx.x < WIDTH && b < a.B) a.runs[i * a.B + b] = make_double2(r.p, r.q);
         } else {
-            const double behind = MODE == 2 ? behind_chunk<kSideThreads, kWidth, DONES>(a, b, i) : 0.0;
-            walk<T, kSideThreads, kWidth, false, DONES, true>(a, b, t0, t1, len, last, behind);
+            const double behind = MODE == 2 ? behind_chunk<kSideThreads, WIDTH, DONES>(a, b, i) : 0.0;
+            walk<T, kSideThreads, WIDTH, false, DONES, true>(a, b, t0, t1, len, last, behind);
         }
     }
 }
@@ -320,21 +318,22 @@ void launch_row(const GaeArgs &a, hipStream_t s)
         hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, DONES, 2>), grid, dim3(kBlock), 0, s, a);
     }
 }
-template <typename T, bool DONES>
+template <typename T, int WIDTH, bool DONES>
 void launch_side(const GaeArgs &a, hipStream_t s)
 {
-    const dim3 grid(blocks_for((a.B + kWidth - 1) / kWidth * a.chunks));
+    const dim3 grid(blocks_for((a.B + WIDTH - 1) / WIDTH * a.chunks)), block(kSideThreads);
     if (a.chunks == 1) {
-        hipLaunchKernelGGL((gae_side_kernel<T, DONES, 0>), grid, dim3(kSideThreads), 0, s, a);
+        hipLaunchKernelGGL((gae_side_kernel<T, WIDTH, DONES, 0>), grid, block, 0, s, a);
     } else {
-        hipLaunchKernelGGL((gae_side_kernel<T, DONES, 1>), grid, dim3(kSideThreads), 0, s, a);
-        hipLaunchKernelGGL((gae_side_kernel<T, DONES, 2>), grid, dim3(kSideThreads), 0, s, a);
+        hipLaunchKernelGGL((gae_side_kernel<T, WIDTH, DONES, 1>), grid, block, 0, s, a);
+        hipLaunchKernelGGL((gae_side_kernel<T, WIDTH, DONES, 2>), grid, block, 0, s, a);
     }
 }
 template <typename T, bool DONES>
 void launch_of(const GaeArgs &a, hipStream_t s)
 {
-    if (a.layout == kGaeSide) launch_side<T, DONES>(a, s);
+    if (a.layout == kGaeSide && a.width == 16) launch_side<T, 16, DONES>(a, s);
+    else if (a.layout == kGaeSide) launch_side<T, 64, DONES>(a, s);
     else if (a.layout == kGaeStrided) launch_row<T, 256, false, DONES>(a, s);
     else if (a.threads == 64) launch_row<T, 64, true, DONES>(a, s);
     else if (a.threads == 256) launch_row<T, 256, true, DONES>(a, s);
@@ -360,10 +359,15 @@ GaePlan plan_gae(int64_t B, int64_t S, int layout)
                 : layout == kGaeStrided ? 256
                 : S <= 64 * kSteps ? 64
                 : S <= 256 * kSteps || B * ((S + 4095) / 4096) < 256 ? 256 : 512;
-    const int64_t tile = layout == kGaeSide ? kSideThreads / kWidth * kSteps : (int64_t)p.threads * kSteps;
-    const int64_t tiles = (S + tile - 1) / tile, units = layout == kGaeSide ? (B + kWidth - 1) / kWidth : B;
+    // Side by side: sixteen trajectories a workgroup and tiles of 256 steps, which few trajectories are cut into; many with more steps than a tile go by 64,
+    // 256 contiguous bytes of each step (fp32, ragged with dones, us at 16 / 64: 726 x 4630 44 / 34, 2048 x 2048 40 / 33; 200 x 8000 19 / 24, 64 x 65536
+    // 29 / 45).  Two tiles are walked in one launch rather than cut (128 x 500 12.1 / 9.6; of four 128 x 1024 12.5 / 15.8).
+    p.width = layout != kGaeSide ? 1 : B >= 512 && S > kSideThreads / 16 * kSteps ? 64 : 16;
+    const int64_t tile = (int64_t)p.threads / p.width * kSteps;
+    const int64_t tiles = (S + tile - 1) / tile, units = (B + p.width - 1) / p.width;
     const int64_t want = units > 0 ? (512 + units - 1) / units : 1;
     int64_t n = want < tiles ? want : tiles;
+    if (p.width == 16 && tiles <= 2) n = 1;
     if (n < 1) n = 1;
     const int64_t per = tiles > 0 ? (tiles + n - 1) / n : 1;
     p.chunk = per * tile;

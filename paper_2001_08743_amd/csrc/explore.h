@@ -55,16 +55,17 @@ struct GaeArgs {
     const int *lengths;
     double gamma, gamma_lambda, factor_eight;      // gamma, gamma lambda, its eighth power
     float *adv, *ret;
-    double2 *runs;                 // [B][chunks] what a chunk makes of the advantage behind it: factor, summand
+    double2 *runs;                 // what a chunk makes of the advantage behind it: factor, summand; [B][chunks], side by side [chunks][B]
     int64_t chunk;                 // steps of a chunk (S rounded up: one chunk)
     int chunks;
-    int threads;                   // of a trajectory
+    int threads;                   // of a workgroup's trajectories
+    int width;                     // trajectories side by side in a wave
     int layout;
 };
 // How trajectories lie in memory: the steps of each one run of items, the same step of all, or neither.
 constexpr int kGaeDense = 0, kGaeSide = 1, kGaeStrided = 2;
 struct GaePlan {
-    int threads, chunks;
+    int threads, width, chunks;
     int64_t chunk, bytes;
 };
 GaePlan plan_gae(int64_t B, int64_t S, int layout);

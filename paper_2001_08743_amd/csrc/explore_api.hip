@@ -213,13 +213,14 @@ int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_
     a.gamma = gamma;
     const double gl = gamma * lambda, gl2 = gl * gl, gl4 = gl2 * gl2;
     a.gamma_lambda = gl;
-    a.factor_eight = gl4 * gl4;
+    a.factor_eight = gl == 0.0 ? 0.0 : fmax(gl4 * gl4, 1e-300);      // 0 stands for an episode's end
     a.adv = advantages;
     a.ret = returns;
     a.runs = static_cast<double2 *>(workspace);
     a.chunk = p.chunk;
     a.chunks = p.chunks;
     a.threads = p.threads;
+    a.width = p.width;
     a.layout = layout;
     const hipError_t h = launch_gae(a, type, reinterpret_cast<hipStream_t>(stream));
     return h == hipSuccess ? CHAM_OK : hip_fail(h);

@@ -289,7 +289,7 @@ def test_binding_refuses():
 
 # --- advantages
 
-GAE_SHAPES = [(1, 1), (3, 2), (128, 500), (1, 2047), (2, 2048), (5, 2049), (70, 64), (130, 33), (300, 7), (1000, 1), (3, 20000), (1, 70001), (17, 9000), (2, 300)]
+GAE_SHAPES = [(1, 1), (3, 2), (128, 500), (1, 2047), (2, 2048), (5, 2049), (70, 64), (130, 33), (300, 7), (1000, 1), (3, 20000), (1, 70001), (17, 9000), (2, 300), (512, 256), (513, 257), (777, 321), (530, 2100)]
 
 
 def _gae_inputs(B, S, dtype, seed):
@@ -348,7 +348,7 @@ def test_gae_steps_behind_a_length_are_not_read_and_lengths_are_held():
     assert torch.equal(only["advantages"], got["advantages"])
 
 
-@pytest.mark.parametrize("B,S,at", [(9, 70, 33), (9, 70, 32), (2, 3000, 1999), (1, 60000, 40000)])
+@pytest.mark.parametrize("B,S,at", [(9, 70, 33), (9, 70, 32), (2, 3000, 1999), (1, 60000, 40000), (600, 700, 300), (8, 400, 127)])
 def test_gae_an_episode_keeps_its_nan(B, S, at):
     i = _gae_inputs(B, S, torch.float32, 91)
     i["dones"][:] = 0
