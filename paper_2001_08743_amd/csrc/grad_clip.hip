@@ -14,24 +14,25 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kPieces = 4;                 // of 16 bytes that a thread asks for at a time
 constexpr int kChunkBytes = kThreads * kPieces * 16;
-constexpr int kMostTensors = 120;          // of a launch: 4 KiB of arguments
-constexpr int kFewTensors = 12;            // of a launch with a tenth of that to write and to copy (a call of six tensors: 11.3 -> 10 us of host time)
+// Tensors of a launch: 4 KiB of arguments.  A launch more is 4 us of host time (191 small tensors in two and two launches 21.6 us, in one and two 16).
+constexpr int kMostRead = 280, kMostScaled = 180;
+constexpr int kFewTensors = 12;            // of a launch with a tenth of that to write and to copy (a call of six tensors: 10.9 -> 10.4 us)
 constexpr int kBlocks = 1024;              // workgroups of all launches of a call together (what is on the chip at a time), but one each at least
 
-template <int MOST>
+template <int MOST, bool OUT>
 struct Tensors {
     const void *from[MOST];
-    void *to[MOST];
-    int64_t numel[MOST];
+    void *to[OUT ? MOST : 1];              // OUT: where the scaled items go
     int first[MOST + 1];                   // chunk at which a tensor begins
-    uint8_t type[MOST];
+    uint16_t tail[MOST];                   // items of a tensor's last chunk less one, times four; and its type
     int n;
 };
-static_assert(sizeof(Tensors<kMostTensors>) <= 4000, "arguments within 4 KiB, with what goes beside them");
+static_assert(kChunkBytes / 2 <= 1 << 14, "a chunk's items less one in fourteen bits");
+static_assert(sizeof(Tensors<kMostRead, false>) <= 4000 && sizeof(Tensors<kMostScaled, true>) <= 4000, "arguments within 4 KiB, with what goes beside them");
 
 // Tensor of a chunk.
-template <int MOST>
-__device__ __forceinline__ int tensor_of(const Tensors<MOST> &t, int chunk)
+template <int MOST, bool OUT>
+__device__ __forceinline__ int tensor_of(const Tensors<MOST, OUT> &t, int chunk)
 {
     int lo = 0, hi = t.n;
     while (hi - lo > 1) {
@@ -99,8 +100,8 @@ __device__ __forceinline__ void chunk_squares(const void *from, int n, double (&
 }
 
 // The chunks [lo, hi) of a block: consecutive ones, so that a tensor is looked up once and then followed.
-template <int MOST>
-__device__ __forceinline__ void share_of(const Tensors<MOST> &t, int &lo, int &hi)
+template <int MOST, bool OUT>
+__device__ __forceinline__ void share_of(const Tensors<MOST, OUT> &t, int &lo, int &hi)
 {
     const int64_t n = t.first[t.n];
     lo = (int)(n * blockIdx.x / gridDim.x);
@@ -109,17 +110,17 @@ __device__ __forceinline__ void share_of(const Tensors<MOST> &t, int &lo, int &h
 
 struct Chunk {
     int64_t at;                            // first item
-    int n;
+    int n, type;
 };
-template <int MOST>
-__device__ __forceinline__ Chunk chunk_of(const Tensors<MOST> &t, int tensor, int chunk)
+template <int MOST, bool OUT>
+__device__ __forceinline__ Chunk chunk_of(const Tensors<MOST, OUT> &t, int tensor, int chunk)
 {
-    const int64_t items = kChunkBytes / (t.type[tensor] == 0 ? 4 : 2), at = (chunk - t.first[tensor]) * items, left = t.numel[tensor] - at;
-    return {at, (int)(left < items ? left : items)};
+    const int tail = t.tail[tensor], type = tail & 3, items = kChunkBytes / (type == 0 ? 4 : 2);
+    return {(int64_t)(chunk - t.first[tensor]) * items, chunk + 1 == t.first[tensor + 1] ? (tail >> 2) + 1 : items, type};
 }
 
 template <int MOST>
-__global__ void __launch_bounds__(kThreads, 8) grad_squares_kernel(const Tensors<MOST> t, double *parts)
+__global__ void __launch_bounds__(kThreads, 8) grad_squares_kernel(const Tensors<MOST, false> t, double *parts)
 {
     double s[4] = {};
     int lo, hi;
@@ -127,8 +128,8 @@ __global__ void __launch_bounds__(kThreads, 8) grad_squares_kernel(const Tensors
     for (int c = lo, i = tensor_of(t, lo); c < hi; ++c) {
         while (c >= t.first[i + 1]) ++i;
         const Chunk k = chunk_of(t, i, c);
-        if (t.type[i] == 0) chunk_squares<F32>(static_cast<const float *>(t.from[i]) + k.at, k.n, s);
-        else if (t.type[i] == 1) chunk_squares<BF16>(static_cast<const __bf16 *>(t.from[i]) + k.at, k.n, s);
+        if (k.type == 0) chunk_squares<F32>(static_cast<const float *>(t.from[i]) + k.at, k.n, s);
+        else if (k.type == 1) chunk_squares<BF16>(static_cast<const __bf16 *>(t.from[i]) + k.at, k.n, s);
         else chunk_squares<F16>(static_cast<const _Float16 *>(t.from[i]) + k.at, k.n, s);
     }
     const double sum = block_sum((s[0] + s[1]) + (s[2] + s[3]));
@@ -179,7 +180,7 @@ __device__ __forceinline__ void chunk_scale(const void *from, void *to, int n, f
 
 // parts: the sums of squares of this call (block 0 of the first launch notes the norm); null: *norm is given.
 template <int MOST>
-__global__ void __launch_bounds__(kThreads, 8) grad_clip_kernel(const Tensors<MOST> t, double max_norm, const double *parts, int n_parts, double *norm, int first)
+__global__ void __launch_bounds__(kThreads, 8) grad_clip_kernel(const Tensors<MOST, true> t, double max_norm, const double *parts, int n_parts, double *norm, int first)
 {
     double v;
     if (parts) {
@@ -197,31 +198,29 @@ __global__ void __launch_bounds__(kThreads, 8) grad_clip_kernel(const Tensors<MO
         while (c < t.first[i]) --i;
         if (whole && t.from[i] == t.to[i]) continue;
         const Chunk k = chunk_of(t, i, c);
-        if (t.type[i] == 0) chunk_scale<F32>(static_cast<const float *>(t.from[i]) + k.at, static_cast<float *>(t.to[i]) + k.at, k.n, f);
-        else if (t.type[i] == 1) chunk_scale<BF16>(static_cast<const __bf16 *>(t.from[i]) + k.at, static_cast<__bf16 *>(t.to[i]) + k.at, k.n, f);
+        if (k.type == 0) chunk_scale<F32>(static_cast<const float *>(t.from[i]) + k.at, static_cast<float *>(t.to[i]) + k.at, k.n, f);
+        else if (k.type == 1) chunk_scale<BF16>(static_cast<const __bf16 *>(t.from[i]) + k.at, static_cast<__bf16 *>(t.to[i]) + k.at, k.n, f);
         else chunk_scale<F16>(static_cast<const _Float16 *>(t.from[i]) + k.at, static_cast<_Float16 *>(t.to[i]) + k.at, k.n, f);
     }
 }
 
-int64_t chunks_in(int64_t numel, int type)
-{
-    const int64_t items = kChunkBytes / type_bytes(type);
-    return (numel + items - 1) / items;
-}
+// Items of a chunk are a power of two: no division for each of many tensors.
+constexpr int shift_of(int type) { return type == 0 ? 13 : 14; }
+static_assert(kChunkBytes == 4 << shift_of(0) && kChunkBytes == 2 << shift_of(1), "items of a chunk");
+int64_t chunks_in(int64_t numel, int type) { return (numel + (int64_t(1) << shift_of(type)) - 1) >> shift_of(type); }
 
 // The tensors from `i` on that go into one launch (empty ones left out); returns the first that does not.
-template <int MOST>
-int gather(Tensors<MOST> &t, int i, const void *const *grads, void *const *outs, const int64_t *numels, const int32_t *types, int n)
+template <int MOST, bool OUT>
+int gather(Tensors<MOST, OUT> &t, int i, const void *const *grads, void *const *outs, const int64_t *numels, const int32_t *types, int n)
 {
     t.n = 0;
     t.first[0] = 0;
     for (; i < n && t.n < MOST; ++i) {
         if (numels[i] == 0) continue;
         t.from[t.n] = grads ? grads[i] : nullptr;
-        t.to[t.n] = outs ? outs[i] : const_cast<void *>(t.from[t.n]);
-        t.numel[t.n] = numels[i];
-        t.type[t.n] = (uint8_t)types[i];
+        if (OUT) t.to[t.n] = outs ? outs[i] : const_cast<void *>(grads[i]);
         const int64_t end = t.first[t.n] + chunks_in(numels[i], types[i]);
+        t.tail[t.n] = (uint16_t)(((numels[i] - 1) & ((int64_t(1) << shift_of(types[i])) - 1)) * 4 + types[i]);
         t.first[++t.n] = (int)end;                 // of 2^40 items at most: below 2^28
     }
     return i;
@@ -235,8 +234,8 @@ int64_t chunks_of(const int64_t *numels, const int32_t *types, int n)
 }
 
 // Workgroups of a launch: one a chunk, or its share of kBlocks.
-template <int MOST>
-int blocks_of(const Tensors<MOST> &t, int64_t all_chunks)
+template <int MOST, bool OUT>
+int blocks_of(const Tensors<MOST, OUT> &t, int64_t all_chunks)
 {
     const int64_t c = t.first[t.n];
     if (all_chunks <= kBlocks || c == 0) return (int)c;
@@ -247,7 +246,7 @@ int blocks_of(const Tensors<MOST> &t, int64_t all_chunks)
 template <int MOST>
 int parts_of(const int64_t *numels, const int32_t *types, int n)
 {
-    Tensors<MOST> t;
+    Tensors<MOST, false> t;
     const int64_t all = chunks_of(numels, types, n);
     int parts = 0;
     for (int i = 0; i < n;) {
@@ -260,7 +259,7 @@ int parts_of(const int64_t *numels, const int32_t *types, int n)
 template <int MOST>
 void launch_squares(const void *const *grads, const int64_t *numels, const int32_t *types, int n, double *parts, hipStream_t s)
 {
-    Tensors<MOST> t;
+    Tensors<MOST, false> t;
     const int64_t all = chunks_of(numels, types, n);
     int at = 0;
     for (int i = 0; i < n;) {
@@ -276,11 +275,15 @@ template <int MOST>
 void launch_scale(const void *const *grads, void *const *outs, const int64_t *numels, const int32_t *types, int n, double max_norm, double *norm,
                   const double *parts, int n_parts, hipStream_t s)
 {
-    Tensors<MOST> t;
+    Tensors<MOST, true> t;
     const int64_t all = chunks_of(numels, types, n);
     int first = 1;
-    for (int i = 0; i < n;) {
-        i = gather(t, i, grads, outs, numels, types, n);
+    // the last tensors first, as the chunks within a launch
+    for (int end = n; end > 0;) {
+        int begin = end;
+        for (int most = MOST; begin > 0 && most > 0; --begin) most -= numels[begin - 1] != 0;
+        gather(t, begin, grads, outs, numels, types, end);
+        end = begin;
         if (t.n == 0) break;
         hipLaunchKernelGGL(grad_clip_kernel<MOST>, dim3((unsigned)blocks_of(t, all)), dim3(kThreads), 0, s, t, max_norm, parts, n_parts, norm, first);
         first = 0;
@@ -291,14 +294,14 @@ void launch_scale(const void *const *grads, void *const *outs, const int64_t *nu
 
 int grad_parts(const int64_t *numels, const int32_t *types, int n)
 {
-    return n <= kFewTensors ? parts_of<kFewTensors>(numels, types, n) : parts_of<kMostTensors>(numels, types, n);
+    return n <= kFewTensors ? parts_of<kFewTensors>(numels, types, n) : parts_of<kMostRead>(numels, types, n);
 }
 
 hipError_t launch_grad_norm(const void *const *grads, const int64_t *numels, const int32_t *types, int n, double *parts, int n_parts,
                             double *norm, hipStream_t s)
 {
     if (n <= kFewTensors) launch_squares<kFewTensors>(grads, numels, types, n, parts, s);
-    else launch_squares<kMostTensors>(grads, numels, types, n, parts, s);
+    else launch_squares<kMostRead>(grads, numels, types, n, parts, s);
     if (norm) hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(kThreads), 0, s, parts, n_parts, norm);
     return hipGetLastError();
 }
@@ -307,7 +310,7 @@ hipError_t launch_grad_clip(const void *const *grads, void *const *outs, const i
                             double max_norm, double *norm, const double *parts, int n_parts, hipStream_t s)
 {
     if (n <= kFewTensors) launch_scale<kFewTensors>(grads, outs, numels, types, n, max_norm, norm, parts, n_parts, s);
-    else launch_scale<kMostTensors>(grads, outs, numels, types, n, max_norm, norm, parts, n_parts, s);
+    else launch_scale<kMostScaled>(grads, outs, numels, types, n, max_norm, norm, parts, n_parts, s);
     return hipGetLastError();
 }
 
