@@ -19,7 +19,7 @@ struct Run {
     double p, q;                          // factor and summand
 };
 // q + p x.  CUT (where episodes end inside): q alone where p is 0, so that an episode takes nothing from the next one, not even a NaN; a factor is
-// then 0 by an episode's end (or gamma lambda = 0), never by underflow.
+// then 0 by an episode's end, never by underflow.
 template <bool CUT>
 __device__ __forceinline__ double apply(double p, double x, double q) { return CUT && p == 0.0 ? q : __builtin_fma(p, x, q); }
 template <bool CUT>
@@ -311,9 +311,9 @@ void launch_row(const GaeArgs &a, hipStream_t s)
 {
     constexpr int kBlock = THREADS < 256 ? 256 : THREADS, kRows = kBlock / THREADS;
     const dim3 grid(blocks_for((a.B * a.chunks + kRows - 1) / kRows));
-    if (a.chunks == 1) {
+    if (THREADS == 64 || a.chunks == 1) {                 // a wave's trajectories are one tile
         hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, DONES, 0>), grid, dim3(kBlock), 0, s, a);
-    } else {
+    } else if constexpr (THREADS > 64) {
         hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, DONES, 1>), grid, dim3(kBlock), 0, s, a);
         hipLaunchKernelGGL((gae_row_kernel<T, THREADS, DENSE, DONES, 2>), grid, dim3(kBlock), 0, s, a);
     }

@@ -211,9 +211,10 @@ int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_
     a.bootstrap = bootstrap;
     a.lengths = lengths;
     a.gamma = gamma;
-    const double gl = gamma * lambda, gl2 = gl * gl, gl4 = gl2 * gl2;
+    // a factor of 0 stands for an episode's end, and for nothing else: 1e-300 times an advantage is below what a float resolves
+    const double gl = fmax(gamma * lambda, 1e-300), gl2 = gl * gl, gl4 = gl2 * gl2;
     a.gamma_lambda = gl;
-    a.factor_eight = gl == 0.0 ? 0.0 : fmax(gl4 * gl4, 1e-300);      // 0 stands for an episode's end
+    a.factor_eight = fmax(gl4 * gl4, 1e-300);
     a.adv = advantages;
     a.ret = returns;
     a.runs = static_cast<double2 *>(workspace);

@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(kThreads) policy_terms_kernel(const PolicyArgs
 
 constexpr int kTileHeads = 1024;                // at most: kHeadsPerThread of each thread
 constexpr int kHeadsPerThread = kTileHeads / kThreads;
-constexpr int kTileItems = 8448;                // fp32 logits in LDS, 33 KiB: four workgroups share a compute unit
+constexpr int kTileItems = 8448;                // fp32 logits in LDS, 33 KiB: with 17 KiB of the heads' three workgroups share a compute unit
 constexpr int kTileChoices = 32;                // beyond, a tile has fewer heads than threads
 constexpr int kLaneChoices = 64;                // what a lane's registers hold
 
@@ -1000,8 +1000,12 @@ void launch_row_of(const PolicyArgs &a, unsigned blocks, hipStream_t s)
 {
     constexpr int kRegisters = N < 8 ? N : 8, kLds = N - kRegisters;
     const dim3 block(THREADS < kThreads ? kThreads : THREADS);
-    if (!a.grad) hipLaunchKernelGGL((policy_row_kernel<T, THREADS, kRegisters, 0, false, false>), dim3(blocks), block, 0, s, a);
-    else if (a.c_entropy != 0.0) hipLaunchKernelGGL((policy_row_kernel<T, THREADS, kRegisters, kLds, true, true>), dim3(blocks), block, 0, s, a);
+    if constexpr (THREADS * N <= kWideRow)                // longer rows without gradients go by parts
+        if (!a.grad) {
+            hipLaunchKernelGGL((policy_row_kernel<T, THREADS, kRegisters, 0, false, false>), dim3(blocks), block, 0, s, a);
+            return;
+        }
+    if (a.c_entropy != 0.0) hipLaunchKernelGGL((policy_row_kernel<T, THREADS, kRegisters, kLds, true, true>), dim3(blocks), block, 0, s, a);
     else hipLaunchKernelGGL((policy_row_kernel<T, THREADS, kRegisters, kLds, true, false>), dim3(blocks), block, 0, s, a);
 }
 template <typename T>

@@ -369,6 +369,20 @@ def test_gae_an_episode_keeps_its_nan(B, S, at):
     assert torch.isnan(binding.cham_gae(r, v, 0.5, 0.5)["advantages"]).all()
 
 
+@pytest.mark.parametrize("gamma,lam", [(0.0, 0.9), (0.9, 0.0)])
+@pytest.mark.parametrize("B,S", [(9, 70), (600, 700), (1, 30000)])
+def test_gae_without_a_sum_behind(B, S, gamma, lam):
+    i = _gae_inputs(B, S, torch.float32, 92)
+    adv, ret, there = ref.gae(i["rewards"], i["values"], gamma, lam, i["dones"], i["bootstrap"], None)
+    for place in (lambda t: t.to(DEV), lambda t: t.to(DEV).t().contiguous().t()):
+        r, v, d = place(i["rewards"]), place(i["values"]), place(i["dones"])
+        _check_gae(binding.cham_gae(r, v, gamma, lam, dones=d, bootstrap=i["bootstrap"].to(DEV)), (adv, ret), there)
+        d.zero_()
+        r[:, S - 1] = math.nan                            # 0 times what is no number is none, with dones or without them
+        for dones in (None, d):
+            assert torch.isnan(binding.cham_gae(r, v, gamma, lam, dones=dones)["advantages"]).all()
+
+
 def test_gae_side_by_side_in_many_chunks():
     B, S = 20, 40001
     i = _gae_inputs(B, S, torch.float32, 77)
