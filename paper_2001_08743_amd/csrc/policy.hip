@@ -1078,7 +1078,11 @@ hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
         const int rows = p.threads < kThreads ? kThreads / p.threads : 1;
         const int64_t groups = (a.R + rows - 1) / rows;
         const int64_t resident = (int64_t)kUnits * (row_waves(p.row) * 4 / (p.threads < kThreads ? kThreads / 64 : p.threads / 64));
-        const unsigned blocks = (unsigned)(groups < resident ? groups : resident);
+        // Log-probabilities alone: a workgroup for every long row, which the hardware spreads better than a fixed share (us, bf16, share / each:
+        // 4096 x 32768 52.2 / 46.5, 16384 x 16384 113 / 101; by waves 6001 x 8191 22.4 / 23.8).  With gradients, whose stores the next row's
+        // loads run under, and a loss's sums, a share (4096 x 131072 440 / 474, 16384 x 1000 22.7 / 26.5).
+        const bool each = !a.old_logp && p.threads >= kThreads;
+        const unsigned blocks = each ? blocks_for(groups) : (unsigned)(groups < resident ? groups : resident);
         if (a.R > 0) launch_row<T>(a, p, blocks, s);
         return launch_terms(a, blocks, s);
     }
