@@ -454,6 +454,25 @@ def test_norm_and_clip_over_sizes(sizes, types, offset):
         assert torch.equal(t, o)
 
 
+def test_norm_and_clip_of_many_chunks():
+    # more than 128 MiB: a workgroup for every 32 KiB scales
+    sizes = [5, 41_000_001, 0, 16384, 16_000_003]
+    types = (torch.bfloat16, torch.bfloat16, torch.float32, torch.float16, torch.float32)
+    g = torch.Generator(device=DEV).manual_seed(6)
+    ts = [torch.randn(n, generator=g, device=DEV).to(t) for n, t in zip(sizes, types)]
+    want = _norm64(ts)
+    outs = [torch.empty_like(t) for t in ts]
+    r = binding.cham_clip_grads(ts, 0.3 * want, out=outs)
+    assert abs(float(r["norm"]) - want) <= want * sum(sizes) * 2.0 ** -52
+    factor = 0.3 * want / (want + 1e-6)
+    for t, o in zip(ts, outs):
+        x = t.double() * factor
+        assert (o.double() - x).abs().le(x.abs() * (2 * ref.U + ref.HALF[t.dtype]) * (1 + 1e-6) + ref.TINY[t.dtype]).all()
+    binding.cham_clip_grads(ts, 0.3 * want)
+    for t, o in zip(ts, outs):
+        assert torch.equal(t, o)
+
+
 def test_norm_of_values_whose_squares_leave_fp32():
     for scale in (1e30, 1e-30):
         ts = _tensors([1000, 77], TYPES[:2], 9, scale=scale)
