@@ -4,7 +4,9 @@
 // maps: steps t .. u make of the advantage behind them q + p A_{u+1}, and two runs (p1, q1), (p2, q2), the second later, join
 // to (p1 p2, q1 + p1 q2).  So every thread folds eight consecutive steps, the runs of a workgroup's threads are scanned from the end,
 // and every thread walks its steps once more with the advantage behind them known: one read of everything, one write.  In
-// double: the sum over a long trajectory keeps its small terms, and the arithmetic is hidden behind memory all the same.
+// double: the sum over a long trajectory keeps its small terms.
+// Bound by latency: a workgroup's loads, its join (shuffles and a barrier) and its stores follow each other (bf16 512 x 8192 ragged
+// 11 us, 2.2 TB/s; fp32 128 x 500 step by step 8.5 us).  Few long trajectories are cut into chunks of their own workgroups and read twice.
 #include "cham_device.h"
 #include "explore.h"
 #include "explore_items.h"

@@ -396,6 +396,8 @@ __device__ __forceinline__ float2 head_of(const PolicyArgs &a, Soft &v, float xa
 // A lane holds HEADS consecutive heads of up to VP choices in registers (four heads of up to four choices, one of up to 64); as many lanes as
 // that takes side by side are a decision, and a wave takes as many decisions as fit (24 heads of 3: six lanes, ten
 // decisions).  Nothing goes through LDS and no wave waits for another.  Choices from V to VP are masked ones.
+// fp32 64000 x 24 x 3 with gradients 18.7 us, of which the vector instructions are 8 and 40 MB of memory 8: the chain of loads, exponentials,
+// shuffles and the decision in double, twice per wave.  The tile kernel below took 24 us, more than 1024 workgroups 21.
 // V = VP is known at compile time up to four, where a lane's heads are one run of items.
 template <typename T>
 __device__ __forceinline__ void read_head(const typename T::item *p, int n, float *x, int vp)
@@ -542,7 +544,8 @@ __global__ void __launch_bounds__(kThreads, VP > 32 ? 2 : VP > 16 ? 3 : 4) polic
     if (a.old_logp) store_sums<kThreads / 64>(a, sum);
 }
 
-// More: the tile's logits in LDS, eight at a time in a thread's registers.
+// More heads: the tile's logits in LDS, eight at a time in a thread's registers; bound by LDS and its four barriers (fp32 4096 x 128 x 10 with
+// gradients 29 us, 1.5 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs a, const TileShape k)
 {
@@ -814,7 +817,9 @@ __global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_w
     if (a.old_logp) store_partials(a, sum, kRows);
 }
 
-// --- any number of heads and choices, in three steps: sums of parts of heads, decisions, gradient
+// --- any number of heads and choices, in three steps: sums of parts of heads, decisions, gradient.  Three launches and a second read; for few
+// rows of long heads bound by latency (fp32 9 x 50021: 4.6, 6.5 and 4.5 us), for many short heads by the instructions around each
+// (bf16 4096 x 24 x 1000 123 us, 3.2 TB/s; x 100 98 us).
 
 // THREADS of a part: a wave of short heads, a workgroup of parts of long ones.
 template <typename T, int THREADS>
