@@ -39,6 +39,7 @@ struct PolicyPlan {
     int lanes;                     // up to four choices a head: lanes of a decision; 0 elsewhere
     int tile;                      // few choices a head: decisions of a tile; 0 elsewhere
     int row, threads;              // one head: 16-byte pieces of a row that each of so many threads holds; 0 elsewhere
+    int group;                     // several heads of many decisions: lanes that take one at a time; 0 elsewhere
     int splits;                    // workgroups a head is split over
     int chunk;                     // choices each of them takes
     int64_t o_sums, o_part, o_head, o_dec, bytes;

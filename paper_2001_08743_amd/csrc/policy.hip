@@ -818,8 +818,8 @@ __global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_w
 }
 
 // --- any number of heads and choices, in three steps: sums of parts of heads, decisions, gradient.  Three launches and a second read; for few
-// rows of long heads bound by latency (fp32 9 x 50021: 4.6, 6.5 and 4.5 us), for many short heads by the instructions around each
-// (bf16 4096 x 24 x 1000 123 us, 3.2 TB/s; x 100 98 us).
+// rows of long heads bound by latency (fp32 9 x 50021: 4.6, 6.5 and 4.5 us), for many by memory and the instructions around each head
+// (bf16 4096 x 24 x 1000 123 us, 3.2 TB/s).
 
 // THREADS of a part: a wave of short heads, a workgroup of parts of long ones.
 template <typename T, int THREADS>
@@ -968,6 +968,106 @@ __global__ void __launch_bounds__(kThreads) policy_grad_kernel(const PolicyArgs 
     }
 }
 
+// --- several heads of more choices, many decisions: a wave takes a decision, sixteen lanes a head
+
+constexpr int kGroup = 16;
+constexpr int kGroupHeads = 256;                 // at most: what LDS holds of the four decisions of a workgroup
+// us a loss, in three steps / so: bf16 4096 x 24 x 100 97 / 32, x 256 91 / 38, x 1000 123 / 144 (fp32 85 / 33, 87 / 55, 236 / 273); fp32 1024 x 24 x 100
+// 30 / 19, 256 x 24 x 100 17 / 19, 512 x 250 x 70 110 / 158: few decisions leave the chip empty.
+constexpr int kGroupChoices = 512, kGroupRows = 1024;
+
+// Maximum and sum over sixteen lanes, in each of them, by rotations.
+__device__ __forceinline__ Soft soft_group(Soft v)
+{
+    float m = v.m;
+    m = fmaxf(m, shifted<0x121, 0xf>(m, m));       // row_ror 1, 2, 4, 8
+    m = fmaxf(m, shifted<0x122, 0xf>(m, m));
+    m = fmaxf(m, shifted<0x124, 0xf>(m, m));
+    m = fmaxf(m, shifted<0x128, 0xf>(m, m));
+    soft_raise(v, m);
+    v.s += shifted<0x121, 0xf>(v.s, 0.0f);
+    v.s += shifted<0x122, 0xf>(v.s, 0.0f);
+    v.s += shifted<0x124, 0xf>(v.s, 0.0f);
+    v.s += shifted<0x128, 0xf>(v.s, 0.0f);
+    v.t += shifted<0x121, 0xf>(v.t, 0.0f);
+    v.t += shifted<0x122, 0xf>(v.t, 0.0f);
+    v.t += shifted<0x124, 0xf>(v.t, 0.0f);
+    v.t += shifted<0x128, 0xf>(v.t, 0.0f);
+    return v;
+}
+
+// A decision's logits are read for the sums and, out of the caches, for the gradient.  A head's pieces of 16 bytes begin at its first item, wherever
+// that lies; what a head leaves of a last piece is read by item.  Bound by the instructions around short heads and by latency (bf16 4096 x 24 x 100
+// with gradients 32 us, 1.2 TB/s).
+template <typename T>
+__global__ void __launch_bounds__(kThreads) policy_group_kernel(const PolicyArgs a)
+{
+    constexpr int kGroups = 64 / kGroup;
+    __shared__ float4 state[kThreads / 64][kGroupHeads];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane / kGroup, l = lane % kGroup;
+    const int n_vec = a.V / T::kVec, tail = n_vec * T::kVec + l;
+    double sum[kPolicySums] = {};
+    for (int64_t r = (int64_t)blockIdx.x * (kThreads / 64) + wave; r < a.R; r += (int64_t)gridDim.x * (kThreads / 64)) {
+        const bool on = counts(a, r);
+        double lp = 0.0, H = 0.0;
+        bool in = false;
+        Given given{};
+        if (lane == 0) given = given_of(a, r, load_plain);
+        if (on)
+            for (int g0 = 0; g0 < a.G; g0 += kGroups) {
+                const int g = g0 + group, c = g < a.G ? choice_of(a, r * a.G + g) : -1;
+                Soft v = soft_none();
+                float xa = 0.0f;
+                if (c >= 0 && c < a.V) {
+                    const typename T::item *p = static_cast<const typename T::item *>(a.logits) + r * a.ld_r + g * a.ld_g;
+                    xa = T::get(p[c]);
+                    Scale k2 = scale_of(v.m);
+                    float end[1] = {-__builtin_inff()};
+                    if (tail < a.V) end[0] = T::get(p[tail]);
+                    for (int i = l; i < n_vec; i += kGroup) {
+                        float x[T::kVec];
+                        const typename T::words w = *reinterpret_cast<const typename T::words *>(p + i * T::kVec);
+                        T::unpack(make_uint4(w.x, w.y, w.z, w.w), x);
+                        soft_add_all(v, k2, x);
+                    }
+                    soft_add_all(v, k2, end);
+                }
+                v = soft_group(v);
+                if (l == 0 && g < a.G) state[wave][g] = join_head(a, c, xa, v, lp, H, in);
+            }
+        lp = wave_sum(lp);
+        H = wave_sum(H);
+        in = __any(in);
+        float2 d = make_float2(0.0f, 0.0f);
+        if (lane == 0) d = decide(a, r, given, in, lp, H, sum);
+        if (!a.grad) continue;
+        d.x = readlane_f(d.x, 0);
+        d.y = readlane_f(d.y, 0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // state, written by other lanes of this wave
+        for (int g = group; g < a.G; g += kGroups) {
+            typename T::item *to = static_cast<typename T::item *>(a.grad) + r * a.gld_r + g * a.gld_g;
+            const typename T::item *p = static_cast<const typename T::item *>(a.logits) + r * a.ld_r + g * a.ld_g;
+            const float4 k = on ? state[wave][g] : make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
+            const int c = __float_as_int(k.w);
+            const Slope f = slope_of(k.x, k.y, logf(k.y), k.z, d);
+            for (int i = l; i < n_vec; i += kGroup) {
+                float x[T::kVec] = {};
+                if (c >= 0) {
+                    const typename T::words w = *reinterpret_cast<const typename T::words *>(p + i * T::kVec);
+                    T::unpack(make_uint4(w.x, w.y, w.z, w.w), x);
+#pragma unroll
+                    for (int j = 0; j < T::kVec; ++j) x[j] = slope_at<true>(f, x[j]) + (i * T::kVec + j == c ? d.x : 0.0f);
+                }
+                const uint4 y = T::pack(x);
+                *reinterpret_cast<typename T::words *>(to + i * T::kVec) = typename T::words{y.x, y.y, y.z, y.w};
+            }
+            if (tail < a.V) to[tail] = T::put(c >= 0 ? slope_at<true>(f, T::get(p[tail])) + (tail == c ? d.x : 0.0f) : 0.0f);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // before the next decision's state
+    }
+    if (a.old_logp) store_sums<kThreads / 64>(a, sum);
+}
+
 constexpr int kJoinBlocks = 1024;
 constexpr int kTileBlocks = 1024;               // what is on the chip at a time
 constexpr int kUnits = 256;                     // compute units
@@ -1091,6 +1191,12 @@ hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
         if (a.R > 0) launch_row<T>(a, p, blocks, s);
         return launch_terms(a, blocks, s);
     }
+    if (p.group) {
+        const int64_t groups = (a.R + kThreads / 64 - 1) / (kThreads / 64);
+        const unsigned blocks = (unsigned)(groups < kTileBlocks ? groups : kTileBlocks);
+        hipLaunchKernelGGL(policy_group_kernel<T>, dim3(blocks), dim3(kThreads), 0, s, a);
+        return launch_terms(a, blocks, s);
+    }
     const int64_t units = a.R * a.G * p.splits;
     const unsigned join = (unsigned)(a.R <= kJoinFew ? 1 : (a.R + 3) / 4 < kJoinBlocks ? (a.R + 3) / 4 : kJoinBlocks);
     if (a.R > 0) {
@@ -1136,6 +1242,11 @@ PolicyPlan plan_policy(int64_t R, int G, int V, int type, bool grad)
         if (p.threads == 512 && p.row < 8) p.row = 8;
         if (p.threads == 1024) p.row = 16;
         p.bytes = (int64_t)kRowBlocks * kPolicySums * 8;
+        return p;
+    }
+    if (G > 1 && G <= kGroupHeads && V <= kGroupChoices && R >= kGroupRows) {
+        p.group = kGroup;
+        p.bytes = (int64_t)kTileBlocks * kPolicySums * 8;
         return p;
     }
     // parts of a head: of at least 4096 choices, until there are 1024 workgroups

@@ -82,7 +82,7 @@ def _check_loss(got, want, G, V):
 
 SHAPES = [(1, 1, 1), (1, 1, 2), (5, 3, 3), (130, 24, 3), (1037, 5, 3), (7, 64, 2), (33, 12, 24), (3, 200, 7), (2, 300, 3), (2, 1100, 4), (2, 1025, 9), (50, 7, 40), (4, 64, 64), (9, 5, 70), (6, 90, 130), (3, 1, 255), (4, 1, 256), (2, 1, 257),
           (17, 1, 1000), (300, 1, 33), (2, 3, 5000), (70, 2, 300), (3, 1, 4097), (5, 1, 8191), (600, 1, 2049), (2, 1, 50021), (1, 1, 131072),
-          (3, 1, 140001), (1, 2, 270000), (600, 1, 33000), (270, 1, 70001), (260, 1, 140003)]
+          (3, 1, 140001), (1, 2, 270000), (600, 1, 33000), (270, 1, 70001), (260, 1, 140003), (1024, 2, 512), (1025, 3, 511), (4099, 2, 65), (1100, 7, 130), (1024, 2, 513), (1024, 256, 66)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=lambda t: str(t)[6:])
@@ -116,7 +116,7 @@ def test_loss_with_and_without_its_terms(R, G, V, use, entropy_coef):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=lambda t: str(t)[6:])
-@pytest.mark.parametrize("R,G,V", [(40, 4, 3), (21, 3, 50), (13, 1, 901), (3, 2, 4100), (4, 1, 20003)])
+@pytest.mark.parametrize("R,G,V", [(40, 4, 3), (21, 3, 50), (13, 1, 901), (3, 2, 4100), (4, 1, 20003), (1027, 3, 70)])
 def test_strides_and_memory_between(R, G, V, dtype):
     x, a = _policy_inputs(R, G, V, dtype, 11, masked=V > 3)
     b = _loss_inputs(x, a, 0, 12)
@@ -139,7 +139,7 @@ def test_strides_and_memory_between(R, G, V, dtype):
         assert (wide[..., :3] == 7).all() and (wide[..., 3 + V:] == 7).all()
 
 
-@pytest.mark.parametrize("R,G,V", [(12, 5, 3), (12, 4, 90), (6, 1, 700), (6, 1, 40001), (6, 2, 9000)])
+@pytest.mark.parametrize("R,G,V", [(12, 5, 3), (12, 4, 90), (6, 1, 700), (6, 1, 40001), (6, 2, 9000), (1026, 5, 90)])
 def test_left_out_heads_and_decisions(R, G, V):
     x, a = _policy_inputs(R, G, V, torch.float32, 21)
     w = torch.full((R,), 0.25)
@@ -171,7 +171,7 @@ def test_left_out_heads_and_decisions(R, G, V):
     _check_policy(got, lp, H, G, V)
 
 
-@pytest.mark.parametrize("R,G,V", [(50, 5, 3), (50, 1, 700), (5, 1, 40001), (5, 2, 9000)])
+@pytest.mark.parametrize("R,G,V", [(50, 5, 3), (50, 1, 700), (5, 1, 40001), (5, 2, 9000), (1026, 5, 90)])
 def test_weights_of_either_sign(R, G, V):
     x, a = _policy_inputs(R, G, V, torch.float32, 23)
     w = torch.randn(R, generator=_gen(24))
@@ -179,7 +179,7 @@ def test_weights_of_either_sign(R, G, V):
     _check_loss(got, want, G, V)
 
 
-@pytest.mark.parametrize("R,G,V", [(9, 5, 3), (9, 1, 700), (5, 1, 40001), (5, 2, 9000)])
+@pytest.mark.parametrize("R,G,V", [(9, 5, 3), (9, 1, 700), (5, 1, 40001), (5, 2, 9000), (1026, 5, 90)])
 def test_what_is_no_number_stays_in_its_decision(R, G, V):
     x, a = _policy_inputs(R, G, V, torch.float32, 31)
     b = _loss_inputs(x, a, 0, 32)
@@ -254,7 +254,7 @@ def test_rows_beyond_32_bit_offsets():
     assert not bad.any()
 
 
-@pytest.mark.parametrize("R,G,V", [(500, 24, 3), (300, 1, 4000), (3, 1, 60001)])
+@pytest.mark.parametrize("R,G,V", [(500, 24, 3), (300, 1, 4000), (3, 1, 60001), (4200, 5, 100)])
 def test_loss_is_the_same_run_to_run_and_on_another_stream(R, G, V):
     x, a = _policy_inputs(R, G, V, torch.float32, 71)
     b = _loss_inputs(x, a, 0, 72)
