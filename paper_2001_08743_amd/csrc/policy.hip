@@ -246,7 +246,7 @@ __device__ __forceinline__ void write_terms(const PolicyArgs &a, const double *v
 
 // A block's sums, from n partial ones in LDS, to the block's place, where policy_terms_kernel joins them; the only block of a launch writes the
 // terms itself.  Ends without a barrier.
-__device__ __forceinline__ void store_partials(const PolicyArgs &a, const double (*lds)[kPolicySums], int n)
+__device__ __forceinline__ void store_partials(const PolicyArgs &a, const double (*lds)[kPolicySums], int n, bool only)
 {
     if (threadIdx.x != 0) return;
     double v[kPolicySums];
@@ -255,7 +255,7 @@ __device__ __forceinline__ void store_partials(const PolicyArgs &a, const double
         v[i] = 0.0;
         for (int w = 0; w < n; ++w) v[i] += lds[w][i];
     }
-    if (gridDim.x == 1) {
+    if (only) {
         write_terms(a, v);
     } else {
 #pragma unroll
@@ -264,7 +264,7 @@ __device__ __forceinline__ void store_partials(const PolicyArgs &a, const double
 }
 
 template <int WAVES>
-__device__ __forceinline__ void store_sums(const PolicyArgs &a, const double (&sum)[kPolicySums])
+__device__ __forceinline__ void store_sums(const PolicyArgs &a, const double (&sum)[kPolicySums], bool only)
 {
     __shared__ double lds[WAVES][kPolicySums];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -274,7 +274,7 @@ __device__ __forceinline__ void store_sums(const PolicyArgs &a, const double (&s
         if (lane == 0) lds[wave][i] = v;
     }
     __syncthreads();
-    store_partials(a, lds, WAVES);
+    store_partials(a, lds, WAVES, only);
 }
 
 // Terms from the blocks' sums, in a fixed order.  Zeros where there are no blocks.
@@ -541,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, VP > 32 ? 2 : VP > 16 ? 3 : 4) polic
                     for (int j = 0; j < VP; ++j) p[u * a.gld_g + j] = T::put(x[u][j]);
         }
     }
-    if (a.old_logp) store_sums<kThreads / 64>(a, sum);
+    if (a.old_logp) store_sums<kThreads / 64>(a, sum, gridDim.x == 1);
 }
 
 // More heads: the tile's logits in LDS, eight at a time in a thread's registers; bound by LDS and its four barriers (fp32 4096 x 128 x 10 with
@@ -624,7 +624,7 @@ __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs 
             for (int i = tid; i < items; i += kThreads) grad[offset(i, a.gld_r, a.gld_g)] = T::put(x[at(i)]);
         __syncthreads();
     }
-    if (a.old_logp) store_sums<kThreads / 64>(a, sum);
+    if (a.old_logp) store_sums<kThreads / 64>(a, sum, gridDim.x == 1);
 }
 
 // --- one head of more choices: a row stays in the registers of a wave or a workgroup between its sums and its gradient
@@ -814,11 +814,11 @@ __global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_w
         now = next;
     }
     __syncthreads();
-    if (a.old_logp) store_partials(a, sum, kRows);
+    if (a.old_logp) store_partials(a, sum, kRows, gridDim.x == 1);
 }
 
-// --- any number of heads and choices, in three steps: sums of parts of heads, decisions, gradient.  Three launches and a second read; for few
-// rows of long heads bound by latency (fp32 9 x 50021: 4.6, 6.5 and 4.5 us), for many by memory and the instructions around each head
+// --- any number of heads and choices, in three steps: sums of parts of heads, decisions, gradient.  Three launches (two for very few
+// rows of one head) and a second read; for few rows of long heads bound by latency (fp32 9 x 50021: 12 us), for many by memory and the instructions around each head
 // (bf16 4096 x 24 x 1000 123 us, 3.2 TB/s).
 
 // THREADS of a part: a wave of short heads, a workgroup of parts of long ones.
@@ -843,6 +843,7 @@ __global__ void __launch_bounds__(kThreads) policy_part_kernel(const PolicyArgs 
         float end[2] = {-__builtin_inff(), -__builtin_inff()};
         if (tid < head) end[0] = T::get(row[lo + tid]);
         if (tid < hi - tail) end[1] = T::get(row[tail + tid]);
+        const float xa = c >= lo && c < hi ? T::get(row[c]) : 0.0f;
         Scale k2 = scale_of(v.m);
         soft_add_all(v, k2, end);
         for (int i = tid; i < n_vec; i += THREADS) {
@@ -857,7 +858,7 @@ __global__ void __launch_bounds__(kThreads) policy_part_kernel(const PolicyArgs 
             if (tid == 0)
                 for (int w = 1; w < THREADS / 64; ++w) v = soft_join(v, lds[w]);
         }
-        if (tid == 0) reinterpret_cast<float4 *>(a.part)[u] = make_float4(v.m, v.s, v.t, 0.0f);
+        if (tid == 0) reinterpret_cast<float4 *>(a.part)[u] = make_float4(v.m, v.s, v.t, xa);
         if (THREADS > 64) __syncthreads();
     }
 }
@@ -878,13 +879,26 @@ __device__ __forceinline__ float4 join_head(const PolicyArgs &a, int c, float x,
     return make_float4(v.m, v.s, le.y, __int_as_float(c));
 }
 
-// A wave per decision.  Heads of one part: a lane each; of several: the heads one after the other, their parts over the lanes.
-template <typename T, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64) policy_join_kernel(const PolicyArgs a, int splits)
+// A head's sums and, as x, its action's logit from its parts, over a wave.  c: its choice, within the choices.
+__device__ __forceinline__ Soft soft_parts(const PolicyArgs &a, int64_t h, int c, int splits, int chunk, float &x)
+{
+    const float4 *parts = reinterpret_cast<const float4 *>(a.part) + h * splits;
+    Soft v = soft_none();
+    x = parts[c / chunk].w;
+    for (int i = threadIdx.x & 63; i < splits; i += 64) {
+        const float4 p = parts[i];
+        v = soft_join(v, {p.x, p.y, p.z});
+    }
+    return soft_wave(v);
+}
+
+// Decisions, a wave each.  Heads of one part: a lane each; of several: the heads one after the other, their parts over the lanes.
+// LAST: nothing reads what a gradient needs of them.
+template <int WAVES, bool LAST>
+__device__ __forceinline__ void join_rows(const PolicyArgs &a, int splits, int chunk, int64_t first, int64_t step, double (&sum)[kPolicySums])
 {
     const int lane = threadIdx.x & 63;
-    double sum[kPolicySums] = {};
-    for (int64_t r = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6); r < a.R; r += (int64_t)gridDim.x * WAVES) {
+    for (int64_t r = first + (threadIdx.x >> 6); r < a.R; r += step) {
         double lp = 0.0, H = 0.0;
         bool in = false;
         const Given given = given_of(a, r, load_plain);        // asked for ahead of the sums
@@ -893,15 +907,10 @@ __global__ void __launch_bounds__(WAVES * 64) policy_join_kernel(const PolicyArg
                 for (int g = lane; g < a.G; g += 64) {
                     const int64_t h = r * a.G + g;
                     const int c = choice_of(a, h);
-                    Soft v = soft_none();
-                    float x = 0.0f;
-                    if (c >= 0 && c < a.V) {
-                        const float4 p = reinterpret_cast<const float4 *>(a.part)[h];
-                        x = T::get(static_cast<const typename T::item *>(a.logits)[r * a.ld_r + g * a.ld_g + c]);
-                        v = {p.x, p.y, p.z};
-                    }
-                    const float4 out = join_head(a, c, x, v, lp, H, in);
-                    if (a.grad) a.head[h] = out;
+                    float4 p = make_float4(kLowest, 0.0f, 0.0f, 0.0f);
+                    if (c >= 0 && c < a.V) p = reinterpret_cast<const float4 *>(a.part)[h];
+                    const float4 out = join_head(a, c, p.w, {p.x, p.y, p.z}, lp, H, in);
+                    if (!LAST && a.grad) a.head[h] = out;
                 }
                 lp = wave_sum(lp);
                 H = wave_sum(H);
@@ -912,45 +921,72 @@ __global__ void __launch_bounds__(WAVES * 64) policy_join_kernel(const PolicyArg
                     const int c = choice_of(a, h);
                     Soft v = soft_none();
                     float x = 0.0f;
-                    if (c >= 0 && c < a.V) {
-                        x = T::get(static_cast<const typename T::item *>(a.logits)[r * a.ld_r + g * a.ld_g + c]);
-                        for (int i = lane; i < splits; i += 64) {
-                            const float4 p = reinterpret_cast<const float4 *>(a.part)[h * splits + i];
-                            v = soft_join(v, {p.x, p.y, p.z});
-                        }
-                        v = soft_wave(v);
-                    }
+                    if (c >= 0 && c < a.V) v = soft_parts(a, h, c, splits, chunk, x);
                     const float4 out = join_head(a, c, x, v, lp, H, in);
-                    if (a.grad && lane == 0) a.head[h] = out;
+                    if (!LAST && a.grad && lane == 0) a.head[h] = out;
                 }
             }
         }
         if (lane == 0) {
             const float2 d = decide(a, r, given, in, lp, H, sum);
-            if (a.grad) a.dec[r] = d;
+            if (!LAST && a.grad) a.dec[r] = d;
         }
     }
-    if (a.old_logp) store_sums<WAVES>(a, sum);
 }
 
-template <typename T, int THREADS>
+template <int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) policy_join_kernel(const PolicyArgs a, int splits, int chunk)
+{
+    double sum[kPolicySums] = {};
+    join_rows<WAVES, false>(a, splits, chunk, (int64_t)blockIdx.x * WAVES, (int64_t)gridDim.x * WAVES, sum);
+    if (a.old_logp) store_sums<WAVES>(a, sum, gridDim.x == 1);
+}
+
+// JOIN (one head, few decisions): there is no join before it.  Every wave joins its row's parts and takes the decision for itself; what decisions
+// write, and the terms, are left to the last workgroup.
+template <typename T, int THREADS, bool JOIN>
 __global__ void __launch_bounds__(kThreads) policy_grad_kernel(const PolicyArgs a, int splits, int chunk)
 {
     constexpr int kParts = kThreads / THREADS;
     const int tid = threadIdx.x % THREADS, group = THREADS == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS) : 0;
+    const int64_t blocks = (int64_t)gridDim.x - JOIN;
+    if (JOIN && blockIdx.x == blocks) {
+        double sum[kPolicySums] = {};
+        join_rows<kThreads / 64, true>(a, splits, chunk, 0, kThreads / 64, sum);
+        store_sums<kThreads / 64>(a, sum, true);
+        return;
+    }
     const int64_t units = a.R * a.G * splits;
-    for (int64_t u = (int64_t)blockIdx.x * kParts + group; u < units; u += (int64_t)gridDim.x * kParts) {
+    for (int64_t u = (int64_t)blockIdx.x * kParts + group; u < units; u += blocks * kParts) {
         const int64_t h = splits == 1 ? u : u / splits, r = a.G == 1 ? h : h / a.G;
         const int g = (int)(h - r * a.G), lo = (int)(u - h * splits) * chunk;
         const int hi = lo + chunk < a.V ? lo + chunk : a.V;
         typename T::item *to = static_cast<typename T::item *>(a.grad) + r * a.gld_r + g * a.gld_g;
-        const float4 k = counts(a, r) ? a.head[h] : make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
+        float4 k = make_float4(0.0f, 0.0f, 0.0f, __int_as_float(-1));
+        float2 d = make_float2(0.0f, 0.0f);
+        if (counts(a, r)) {
+            if (JOIN) {
+                PolicyArgs quiet = a;
+                quiet.logp = quiet.entropy = quiet.grad_values = nullptr;
+                double lp = 0.0, H = 0.0, sum[kPolicySums] = {};
+                bool in = false;
+                const int c = choice_of(a, h);
+                const Given given = given_of(a, r, load_plain);
+                Soft v = soft_none();
+                float x = 0.0f;
+                if (c >= 0 && c < a.V) v = soft_parts(a, h, c, splits, chunk, x);
+                k = join_head(a, c, x, v, lp, H, in);
+                d = decide(quiet, r, given, in, lp, H, sum);
+            } else {
+                k = a.head[h];
+                d = a.dec[r];
+            }
+        }
         const int c = __float_as_int(k.w);
         if (c < 0) {
             for (int v = lo + tid; v < hi; v += THREADS) to[v] = T::put(0.0f);
             continue;
         }
-        const float2 d = a.dec[r];
         const typename T::item *row = static_cast<const typename T::item *>(a.logits) + r * a.ld_r + g * a.ld_g;
         const Slope f = slope_of(k.x, k.y, logf(k.y), k.z, d);
         const int head = (int)items_to_boundary<T>(row + lo, hi - lo), n_vec = (hi - lo - head) / T::kVec, tail = lo + head + n_vec * T::kVec;
@@ -1065,7 +1101,7 @@ __global__ void __launch_bounds__(kThreads) policy_group_kernel(const PolicyArgs
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // before the next decision's state
     }
-    if (a.old_logp) store_sums<kThreads / 64>(a, sum);
+    if (a.old_logp) store_sums<kThreads / 64>(a, sum, gridDim.x == 1);
 }
 
 constexpr int kJoinBlocks = 1024;
@@ -1073,7 +1109,9 @@ constexpr int kTileBlocks = 1024;               // what is on the chip at a time
 constexpr int kUnits = 256;                     // compute units
 constexpr int kRowBlocks = 6 * kUnits;
 constexpr int kWaveChunk = 2048;                // choices of a part that a wave takes
-constexpr int kJoinFew = 16;                    // decisions that one workgroup joins, a wave each
+// Decisions that one workgroup joins, a wave each; with gradients of one head, beside the gradient's workgroups (us a loss, three launches / two: fp32 1 x 50021
+// 12.7 / 9.1, 9 x 50021 14.0 / 12.2, 16 x 131072 15.5 / 15.5, 32 x 131072 18.0 / 23.7).
+constexpr int kJoinFew = 16;
 
 // A wave or a workgroup per row, by its pieces of 16 bytes: 64 threads up to 1024 pieces (four rows a workgroup, no barrier), 256 up to
 // 4096, 512 to 8192, 1024 beyond, up to sixteen pieces a thread, of which eight in registers and eight in LDS (sixteen in registers: bf16 8192 x
@@ -1198,16 +1236,21 @@ hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
         return launch_terms(a, blocks, s);
     }
     const int64_t units = a.R * a.G * p.splits;
+    const bool fused = a.grad && a.G == 1 && a.R <= kJoinFew;
     const unsigned join = (unsigned)(a.R <= kJoinFew ? 1 : (a.R + 3) / 4 < kJoinBlocks ? (a.R + 3) / 4 : kJoinBlocks);
     if (a.R > 0) {
         const bool wave = p.chunk <= kWaveChunk;
-        const dim3 grid(blocks_for(wave ? (units + 3) / 4 : units));
-        if (wave) hipLaunchKernelGGL((policy_part_kernel<T, 64>), grid, dim3(kThreads), 0, s, a, p.splits, p.chunk);
-        else hipLaunchKernelGGL((policy_part_kernel<T, kThreads>), grid, dim3(kThreads), 0, s, a, p.splits, p.chunk);
-        if (join == 1) hipLaunchKernelGGL((policy_join_kernel<T, kJoinFew>), dim3(1), dim3(kJoinFew * 64), 0, s, a, p.splits);
-        else hipLaunchKernelGGL((policy_join_kernel<T, kThreads / 64>), dim3(join), dim3(kThreads), 0, s, a, p.splits);
-        if (a.grad && wave) hipLaunchKernelGGL((policy_grad_kernel<T, 64>), grid, dim3(kThreads), 0, s, a, p.splits, p.chunk);
-        else if (a.grad) hipLaunchKernelGGL((policy_grad_kernel<T, kThreads>), grid, dim3(kThreads), 0, s, a, p.splits, p.chunk);
+        const dim3 grid(blocks_for(wave ? (units + 3) / 4 : units)), more(grid.x + 1), block(kThreads);
+        if (wave) hipLaunchKernelGGL((policy_part_kernel<T, 64>), grid, block, 0, s, a, p.splits, p.chunk);
+        else hipLaunchKernelGGL((policy_part_kernel<T, kThreads>), grid, block, 0, s, a, p.splits, p.chunk);
+        if (fused) {
+            hipLaunchKernelGGL((policy_grad_kernel<T, kThreads, true>), more, block, 0, s, a, p.splits, p.chunk);
+            return hipGetLastError();
+        }
+        if (join == 1) hipLaunchKernelGGL(policy_join_kernel<kJoinFew>, dim3(1), dim3(kJoinFew * 64), 0, s, a, p.splits, p.chunk);
+        else hipLaunchKernelGGL(policy_join_kernel<kThreads / 64>, dim3(join), block, 0, s, a, p.splits, p.chunk);
+        if (a.grad && wave) hipLaunchKernelGGL((policy_grad_kernel<T, 64, false>), grid, block, 0, s, a, p.splits, p.chunk);
+        else if (a.grad) hipLaunchKernelGGL((policy_grad_kernel<T, kThreads, false>), grid, block, 0, s, a, p.splits, p.chunk);
     }
     return launch_terms(a, join, s);
 }

@@ -116,7 +116,7 @@ def test_loss_with_and_without_its_terms(R, G, V, use, entropy_coef):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=lambda t: str(t)[6:])
-@pytest.mark.parametrize("R,G,V", [(40, 4, 3), (21, 3, 50), (13, 1, 901), (3, 2, 4100), (4, 1, 20003), (1027, 3, 70)])
+@pytest.mark.parametrize("R,G,V", [(40, 4, 3), (21, 3, 50), (13, 1, 901), (3, 2, 4100), (4, 1, 20003), (1027, 3, 70), (5, 1, 70001), (20, 1, 70001)])
 def test_strides_and_memory_between(R, G, V, dtype):
     x, a = _policy_inputs(R, G, V, dtype, 11, masked=V > 3)
     b = _loss_inputs(x, a, 0, 12)
