@@ -23,18 +23,10 @@ constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
 __device__ __forceinline__ float exp2_fast(float z) { return __builtin_amdgcn_exp2f(z); }
 
-// Exponents are taken to the base 2: z = x k - m k, k = log2 e, one fused operation and no rounding but its own; the
-// rounding of m k is common to a head's exponentials and drops out.  Where m k would overflow k is 1: logits that far out are
-// alike or 2^103 apart.
-struct Scale {
-    float k, mk;
-};
-__device__ __forceinline__ Scale scale_of(float m)
-{
-    const float k = fabsf(m) > 1e38f ? 1.0f : kLog2e;
-    return {k, m * k};
-}
-__device__ __forceinline__ float exponent(float x, const Scale &k) { return __builtin_fmaf(x, k.k, -k.mk); }
+// Exponents are taken to the base 2: z = (x - m) log2 e.  The difference comes first, rounded relative to itself, so that no result depends on
+// where a head's logits lie.  (x log2 e - m log2 e in one fused operation saves an instruction but carries the rounding of m log2 e, half a
+// step of a number that may be far from 0, into every exponential: three equal logits of -1e9 were 2^18 apart from their sum.)
+__device__ __forceinline__ float exponent(float x, float m) { return (x - m) * kLog2e; }
 
 // Running maximum and sums of a head: of 2^z and of z 2^z.
 struct Soft {
@@ -51,26 +43,23 @@ __device__ __forceinline__ void soft_raise(Soft &a, float m)
         a.m = m;
     }
 }
-__device__ __forceinline__ void soft_add(Soft &a, float x, const Scale &k)
+__device__ __forceinline__ void soft_add(Soft &a, float x)
 {
-    const float z = exponent(x, k), e = exp2_fast(z);
+    const float z = exponent(x, a.m), e = exp2_fast(z);
     a.s += e;
     a.t = __builtin_fmaf(e, fmaxf(z, kFar), a.t);
 }
-// N items more; k = scale_of(a.m).  m is raised when an item is more than 8 above it and not before: e^8 times V stays far inside
-// fp32, and lanes that each find a new maximum now and then would have the wave rescale all the time.
+// N items more.  m is raised when an item is more than 8 above it and not before: e^8 times V (e^16 V where the sum a.m + 8 is rounded up) stays far
+// inside fp32, and lanes that each find a new maximum now and then would have the wave rescale all the time.
 template <int N>
-__device__ __forceinline__ void soft_add_all(Soft &a, Scale &k, const float (&x)[N])
+__device__ __forceinline__ void soft_add_all(Soft &a, const float (&x)[N])
 {
     float m = x[0];
 #pragma unroll
     for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
-    if (m > a.m + 8.0f) {
-        soft_raise(a, m);
-        k = scale_of(a.m);
-    }
+    if (m > a.m + 8.0f) soft_raise(a, m);
 #pragma unroll
-    for (int j = 0; j < N; ++j) soft_add(a, x[j], k);
+    for (int j = 0; j < N; ++j) soft_add(a, x[j]);
 }
 __device__ __forceinline__ Soft soft_join(Soft a, Soft b)
 {
@@ -89,18 +78,17 @@ __device__ __forceinline__ float2 log_and_entropy(const Soft &v)
 
 // Gradient by a head's logits: 2^z (c0 + c1 z), and D more at the action.
 struct Slope {
-    Scale k;
-    float c0, c1;
+    float m, c0, c1;
 };
 __device__ __forceinline__ Slope slope_of(float m, float s, float ls, float entropy, float2 d)
 {
-    const float inv = __builtin_amdgcn_rcpf(s);              // within an ulp; s is at least e^-8 and at most e^8 V
-    return {scale_of(m), (d.y * (entropy - ls) - d.x) * inv, d.y * kLn2 * inv};
+    const float inv = __builtin_amdgcn_rcpf(s);              // within an ulp; s is at least 1 and at most e^16 V
+    return {m, (d.y * (entropy - ls) - d.x) * inv, d.y * kLn2 * inv};
 }
 template <bool ENT>
 __device__ __forceinline__ float slope_at(const Slope &f, float x)
 {
-    const float z = exponent(x, f.k), e = exp2_fast(z);
+    const float z = exponent(x, f.m), e = exp2_fast(z);
     return ENT ? e * __builtin_fmaf(fmaxf(z, kFar), f.c1, f.c0) : e * f.c0;
 }
 
@@ -494,9 +482,8 @@ __global__ void __launch_bounds__(kThreads, VP > 32 ? 2 : VP > 16 ? 3 : 4) polic
                 v[u].m = fmaxf(v[u].m, x[u][j]);
                 xa = j == c[u] ? x[u][j] : xa;
             }
-            const Scale k2 = scale_of(v[u].m);
 #pragma unroll
-            for (int j = 0; j < VP; ++j) soft_add(v[u], x[u][j], k2);
+            for (int j = 0; j < VP; ++j) soft_add(v[u], x[u][j]);
             const float2 one = head_of(a, v[u], xa, c[u], le[u]);
             lp += (double)one.x;
             H += (double)one.y;
@@ -589,12 +576,11 @@ __global__ void __launch_bounds__(kThreads) policy_tile_kernel(const PolicyArgs 
             le[u] = make_float2(0.0f, 0.0f);
             if (h >= heads) continue;
             const float *xh = x + h * k.stride;
-            Scale k2 = scale_of(v[u].m);
             for (int j0 = 0; j0 < a.V; j0 += 8) {
                 float y[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[j] = j0 + j < a.V ? xh[j0 + j] : -__builtin_inff();
-                soft_add_all(v[u], k2, y);
+                soft_add_all(v[u], y);
             }
             const float xa = c[u] >= 0 && c[u] < a.V ? xh[c[u]] : 0.0f;
             t.one[h] = head_of(a, v[u], xa, c[u], le[u]);
@@ -730,7 +716,6 @@ __global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_w
         const Given given = given_of(a, r, load_shared);
         Soft v = soft_none();
         if (c >= 0) {
-            Scale k2 = scale_of(v.m);
             uint4 rest[L > 0 ? L : 1];
 #pragma unroll
             for (int l = 0; l < L; ++l) {
@@ -742,7 +727,7 @@ __global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_w
                 if (k * THREADS < n_vec) {               // of all threads
                     float x[T::kVec];
                     T::unpack(held[k], x);
-                    soft_add_all(v, k2, x);
+                    soft_add_all(v, x);
                 }
                 if (!GRAD) ask(r + step, next, k);
                 else keep_packed(held[k]);
@@ -752,15 +737,15 @@ __global__ void __launch_bounds__(THREADS < kThreads ? kThreads : THREADS, row_w
                 if ((N + l) * THREADS < n_vec) {
                     float x[T::kVec];
                     T::unpack(rest[l], x);
-                    soft_add_all(v, k2, x);
+                    soft_add_all(v, x);
                     if (GRAD) stash[l][threadIdx.x] = rest[l];
                 }
             for (int i = tid + kHeld; i < n_vec; i += THREADS) {
                 float x[T::kVec];
                 T::unpack(body[i], x);
-                soft_add_all(v, k2, x);
+                soft_add_all(v, x);
             }
-            soft_add_all(v, k2, end);
+            soft_add_all(v, end);
         } else if (!GRAD) {
 #pragma unroll
             for (int k = 0; k < N; ++k) ask(r + step, next, k);
@@ -844,12 +829,11 @@ __global__ void __launch_bounds__(kThreads) policy_part_kernel(const PolicyArgs 
         if (tid < head) end[0] = T::get(row[lo + tid]);
         if (tid < hi - tail) end[1] = T::get(row[tail + tid]);
         const float xa = c >= lo && c < hi ? T::get(row[c]) : 0.0f;
-        Scale k2 = scale_of(v.m);
-        soft_add_all(v, k2, end);
+        soft_add_all(v, end);
         for (int i = tid; i < n_vec; i += THREADS) {
             float x[T::kVec];
             T::unpack(body[i], x);
-            soft_add_all(v, k2, x);
+            soft_add_all(v, x);
         }
         v = soft_wave(v);
         if (THREADS > 64) {
@@ -1057,16 +1041,15 @@ __global__ void __launch_bounds__(kThreads) policy_group_kernel(const PolicyArgs
                 if (c >= 0 && c < a.V) {
                     const typename T::item *p = static_cast<const typename T::item *>(a.logits) + r * a.ld_r + g * a.ld_g;
                     xa = T::get(p[c]);
-                    Scale k2 = scale_of(v.m);
                     float end[1] = {-__builtin_inff()};
                     if (tail < a.V) end[0] = T::get(p[tail]);
                     for (int i = l; i < n_vec; i += kGroup) {
                         float x[T::kVec];
                         const typename T::words w = *reinterpret_cast<const typename T::words *>(p + i * T::kVec);
                         T::unpack(make_uint4(w.x, w.y, w.z, w.w), x);
-                        soft_add_all(v, k2, x);
+                        soft_add_all(v, x);
                     }
-                    soft_add_all(v, k2, end);
+                    soft_add_all(v, end);
                 }
                 v = soft_group(v);
                 if (l == 0 && g < a.G) state[wave][g] = join_head(a, c, xa, v, lp, H, in);
