@@ -422,8 +422,8 @@ typedef struct cham_policy_coef {
  *   grad_values DEVICE float [R] or NULL
  * No other output shares memory with an input or another output.
  * The gradient of a minimum or maximum is that of the unclipped side where both are equal.  A term whose coefficient is
- * 0 adds nothing to the total or the gradients, whatever its value.  Exponentials are taken in fp32; differences, products
- * and sums per decision and over decisions in double.
+ * 0 adds nothing to the total or the gradients, whatever its value.  Exponentials are taken in fp32, those of a ratio and a
+ * divergence with the range of a double; differences, products and sums per decision and over decisions in double.
  * Errors: as cham_policy_logp, CHAM_E_BAD_COEF.
  */
 int32_t cham_policy_loss(const void *logits, int32_t type, int64_t R, int32_t G, int32_t V, int64_t ld_r, int64_t ld_g,

@@ -5,9 +5,11 @@
 // H = log s - t / s.  Per decision, lp = sum over heads of log p_action, and with ratio rho = e^(lp - old)
 //   L = w (-min(rho A, clip(rho) A) + c_v value - c_H H + c_kl (e^d - d - 1)),   d = ref - lp
 //   dL/dlp = D = w (-rho A [unclipped side] + c_kl (1 - e^d)),   dL/dx_v = D ([v = a] - p_v) + w c_H p_v (log p_v + H).
-// Exponentials are fp32 (logits have at most 24 bits), and the sums of a head; differences, products and sums per decision and
-// beyond are double.  Double exponentials would change nothing that a log-probability from fp32 sums does not blur, and their
-// constants, held in registers across the rows of a workgroup, took 60 registers of the kernels that hold a row.
+// Exponentials are fp32 (logits have at most 24 bits), and so are the sums of a head, its reciprocal (within an ulp) and, where one lane has a whole
+// head, its log-probability; differences, products and sums per decision and beyond are double, with the ratio's and the divergence's exponential of fp32's
+// significand and double's range.  Double exp and expm1 there would change nothing that a log-probability from fp32 sums does not
+// blur, and their constants spill registers (us a loss, so / with them: 64000 x 24 x 3 20.5 / 21.7, 16384 x 1000 29.6 / 38.0, bf16 4096 x 131072 433 / 485,
+// 4096 x 24 x 100 31.8 / 32.3).
 #include "cham_device.h"
 #include "explore.h"
 #include "explore_items.h"
@@ -138,21 +140,37 @@ __device__ __forceinline__ int choice_of(const PolicyArgs &a, int64_t i)
 
 __device__ __forceinline__ bool counts(const PolicyArgs &a, int64_t r) { return !a.weights || a.weights[r] != 0.0f; }
 
-// e^d - 1 - d, e = e^d - 1.  Near 0 by its series, which loses nothing to the difference (|d| <= 1/4: the first term left out is
-// below 2^-24 of the sum).
-__device__ __forceinline__ float divergence(float d, float e)
+// e^x with the significand of an fp32 exponential (within two steps) and the range of a double: ratios beyond 2^127 are ordinary numbers as long as
+// their products are.
+__device__ __forceinline__ double exp_wide(double x)
 {
-    if (fabsf(d) <= 0.25f) {
+    double z = x * 1.4426950408889634;
+    z = z > 1200.0 ? 1200.0 : z < -1200.0 ? -1200.0 : z;          // infinite, 0; a NaN stays
+    const double n = rint(z);
+    return ldexp((double)exp2_fast((float)(z - n)), z == z ? (int)n : 0);
+}
+
+// e^d - 1 and e^d - 1 - d.  Near 0 by their series, which lose nothing to the difference (|d| <= 1/4: the first term left out is
+// below 2^-24 of the sum).
+struct Gap {
+    double less1, rest;
+};
+__device__ __forceinline__ Gap gap_of(double d)
+{
+    if (fabs(d) <= 0.25) {
+        const float f = (float)d;
         float p = 1.0f / 40320.0f;
-        p = __builtin_fmaf(p, d, 1.0f / 5040.0f);
-        p = __builtin_fmaf(p, d, 1.0f / 720.0f);
-        p = __builtin_fmaf(p, d, 1.0f / 120.0f);
-        p = __builtin_fmaf(p, d, 1.0f / 24.0f);
-        p = __builtin_fmaf(p, d, 1.0f / 6.0f);
-        p = __builtin_fmaf(p, d, 0.5f);
-        return p * d * d;
+        p = __builtin_fmaf(p, f, 1.0f / 5040.0f);
+        p = __builtin_fmaf(p, f, 1.0f / 720.0f);
+        p = __builtin_fmaf(p, f, 1.0f / 120.0f);
+        p = __builtin_fmaf(p, f, 1.0f / 24.0f);
+        p = __builtin_fmaf(p, f, 1.0f / 6.0f);
+        p = __builtin_fmaf(p, f, 0.5f);
+        const double rest = (double)p * d * d;
+        return {d + rest, rest};
     }
-    return e < __builtin_inff() ? e - d : e;           // an action that the policy has lost: infinite, not inf - inf
+    const double e = exp_wide(d);
+    return {e - 1.0, e < __builtin_inf() ? e - 1.0 - d : e};      // an action that the policy has lost: infinite, not inf - inf
 }
 
 // What a decision is compared with.
@@ -191,7 +209,7 @@ __device__ __forceinline__ float2 decide(const PolicyArgs &a, int64_t r, const G
     }
     const double w = a.weights ? (double)in.w : a.w_all;
     const double A = (double)in.adv;
-    const double rho = (double)expf((float)(lp - (double)in.old));
+    const double rho = exp_wide(lp - (double)in.old);
     const double held_rho = rho < a.lo ? a.lo : rho > a.hi ? a.hi : rho;
     const double free = rho * A, held = held_rho * A;
     const bool clipped = free > held;
@@ -213,9 +231,9 @@ __device__ __forceinline__ float2 decide(const PolicyArgs &a, int64_t r, const G
     }
     sum[2] += w * H;
     if (a.ref) {
-        const float d = (float)((double)in.ref - lp), e = expm1f(d);
-        sum[3] += w * (double)divergence(d, e);
-        if (a.c_kl != 0.0) D -= a.c_kl * (double)e;
+        const Gap gap = gap_of((double)in.ref - lp);
+        sum[3] += w * gap.rest;
+        if (a.c_kl != 0.0) D -= a.c_kl * gap.less1;
     }
     if (clipped) sum[4] += w;
     return make_float2((float)(w * D), (float)(w * a.c_entropy));
