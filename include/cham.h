@@ -441,7 +441,8 @@ int64_t cham_gae_workspace_bytes(int64_t B, int64_t S);
  * Advantages (generalised advantage estimation) and returns of B trajectories of up to S steps:
  *   delta_t = r_t + gamma n_t V_{t+1} - V_t,  A_t = delta_t + gamma lambda n_t A_{t+1},  ret_t = A_t + V_t,
  * n_t = 0 where done_t is set and 1 elsewhere, V behind the last step = bootstrap, A behind it = 0.  A step with done_t set
- * takes nothing from behind it, not even a NaN; elsewhere what is no number goes to all earlier steps of its episode.
+ * takes nothing from behind it, not even a NaN; elsewhere what is no number goes to all earlier steps of its episode, an
+ * infinity as one (also where gamma or lambda is 0).
  *   rewards, values DEVICE of `type` (f32, bf16, f16): step s of trajectory b at [b*ld_b + s*ld_s], any strides >= 0
  *   dones     DEVICE uint8, same addressing, or NULL (no episode ends inside)
  *   bootstrap DEVICE float [B] or NULL (zeros): value of the state behind the last step

@@ -20,12 +20,12 @@ constexpr int kSteps = 8;                 // consecutive steps of a thread
 struct Run {
     double p, q;                          // factor and summand
 };
-// q + p x.  CUT (where episodes end inside): q alone where p is 0, so that an episode takes nothing from the next one, not even a NaN; a factor is
-// then 0 by an episode's end, never by underflow.
+// q + p x.  CUT (where episodes end inside): q alone where p is 0, so that an episode takes nothing from the next one, not even a NaN.
+// A factor is 0 by an episode's end, never by underflow: it stays at 1e-300, so that an infinity behind a run is one in front of it.
 template <bool CUT>
 __device__ __forceinline__ double apply(double p, double x, double q) { return CUT && p == 0.0 ? q : __builtin_fma(p, x, q); }
 template <bool CUT>
-__device__ __forceinline__ double factor_join(double a, double b) { return CUT ? a == 0.0 || b == 0.0 ? 0.0 : fmax(a * b, 1e-300) : a * b; }
+__device__ __forceinline__ double factor_join(double a, double b) { return CUT && (a == 0.0 || b == 0.0) ? 0.0 : fmax(a * b, 1e-300); }
 template <bool CUT>
 __device__ __forceinline__ Run run_join(const Run &first, const Run &later) { return {factor_join<CUT>(first.p, later.p), apply<CUT>(first.p, later.q, first.q)}; }
 __device__ __forceinline__ Run run_down(const Run &r, int by) { return {__shfl_down(r.p, by), __shfl_down(r.q, by)}; }
