@@ -473,7 +473,8 @@ int64_t cham_grad_workspace_bytes(const int64_t *numels, const int32_t *types, i
  *          CHAM_TYPE_F32 / BF16 / F16 each; every tensor contiguous, aligned to its items
  *   norm   DEVICE double: sqrt of the sum of all squares, squares and sums in double (no square overflows or vanishes)
  * cham_clip_grads then scales every gradient by max_norm / (norm + 1e-6) unless norm + 1e-6 <= max_norm; gradients are
- * multiplied in fp32 and rounded once.  A NaN norm makes every gradient NaN, an infinite one makes finite gradients 0.
+ * multiplied in fp32 (by a factor below its normal numbers in double) and rounded once.  A NaN norm makes every gradient NaN, an
+ * infinite one makes finite gradients 0.
  *   outs   HOST array of n DEVICE pointers: where the clipped gradients go (an unclipped copy where nothing is clipped);
  *          NULL: in place (not written at all where nothing is clipped).  outs[i] may be grads[i]; otherwise no two tensors
  *          of the call share memory

@@ -150,19 +150,31 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double *parts
     if (threadIdx.x == 0) *norm = v;
 }
 
+// The factor, and what is multiplied: in fp32, or, by a factor that fp32 has no normal number for, in double.
+struct Factor {
+    double wide;
+    float f;
+    bool far;
+};
+
 template <typename T>
-__device__ __forceinline__ void scale_piece(typename T::item *q, int i, const uint4 &raw, float f)
+__device__ __forceinline__ void scale_piece(typename T::item *q, int i, const uint4 &raw, const Factor &f)
 {
     float x[T::kVec];
     T::unpack(raw, x);
+    if (f.far) {
 #pragma unroll
-    for (int j = 0; j < T::kVec; ++j) x[j] *= f;
+        for (int j = 0; j < T::kVec; ++j) x[j] = (float)((double)x[j] * f.wide);
+    } else {
+#pragma unroll
+        for (int j = 0; j < T::kVec; ++j) x[j] *= f.f;
+    }
     const uint4 v = T::pack(x);
     const typename T::words w = {v.x, v.y, v.z, v.w};
     __builtin_nontemporal_store(w, reinterpret_cast<typename T::words *>(q + i * T::kVec));
 }
 template <typename T>
-__device__ __forceinline__ void chunk_scale(const void *from, void *to, int n, float f)
+__device__ __forceinline__ void chunk_scale(const void *from, void *to, int n, const Factor &f)
 {
     const typename T::item *p = static_cast<const typename T::item *>(from);
     typename T::item *q = static_cast<typename T::item *>(to);
@@ -176,7 +188,7 @@ __device__ __forceinline__ void chunk_scale(const void *from, void *to, int n, f
 #pragma unroll
     for (int k = 0; k < kPieces; ++k)
         if (tid + k * kThreads < n_vec) scale_piece<T>(q, tid + k * kThreads, held[k], f);
-    if (at < n) q[at] = T::put(T::get(last) * f);
+    if (at < n) q[at] = T::put(f.far ? (float)((double)T::get(last) * f.wide) : T::get(last) * f.f);
 }
 
 // parts: the sums of squares of this call (block 0 of the first launch notes the norm); null: *norm is given.
@@ -191,7 +203,8 @@ __global__ void __launch_bounds__(kThreads, 8) grad_clip_kernel(const Tensors<MO
         v = *norm;
     }
     const bool whole = v + 1e-6 <= max_norm;
-    const float f = whole ? 1.0f : (float)(max_norm / (v + 1e-6));
+    const double wide = whole ? 1.0 : max_norm / (v + 1e-6);
+    const Factor f{wide, (float)wide, wide < 0x1p-126 && wide > 0.0};
     int lo, hi;
     share_of(t, lo, hi);
     // from the last chunk to the first: what the sum of squares has read last is still in cache
