@@ -19,6 +19,7 @@ constexpr int kChunkBytes = kThreads * kPieces * 16;
 constexpr int kMostRead = 280, kMostScaled = 180;
 constexpr int kFewTensors = 12;            // of a launch with a tenth of that to write and to copy (a call of six tensors: 10.9 -> 10.4 us)
 constexpr int kBlocks = 1024;              // workgroups that sum squares, of all launches of a call together (what is on the chip at a time), one each at least
+constexpr int kMostBlocks = 1 << 20;       // of a launch: 2^32 threads are refused (32 GiB of chunks; beyond, a workgroup takes several)
 
 template <int MOST, bool OUT>
 struct Tensors {
@@ -301,7 +302,7 @@ void launch_scale(const void *const *grads, void *const *outs, const int64_t *nu
         if (t.n == 0) break;
         // Many chunks: a workgroup each, so that the chip walks through memory in order (us a call, spans of kBlocks / one each: 2.7 GB
         // 1580 / 1383, 640 MB 352 / 300, 150 MB 83 / 80).  80 MB, which the caches hold, 41 / 45: the end of a span is still there.
-        const int blocks = all > 4 * kBlocks ? t.first[t.n] : blocks_of(t, all);
+        const int chunks = t.first[t.n], blocks = all <= 4 * kBlocks ? blocks_of(t, all) : chunks < kMostBlocks ? chunks : kMostBlocks;
         hipLaunchKernelGGL(grad_clip_kernel<MOST>, dim3((unsigned)blocks), dim3(kThreads), 0, s, t, max_norm, parts, n_parts, norm, first);
         first = 0;
     }
