@@ -382,7 +382,8 @@ int64_t cham_policy_workspace_bytes(int64_t R, int32_t G, int32_t V, int32_t typ
  * decision with no head left is left out.  An action at or above first_action + V, and a NaN or +inf among a head's logits,
  * give NaN.  Exponentials and their sums are taken in fp32, sums over heads in double.
  * Errors: CHAM_E_NULL, CHAM_E_BAD_DIM (R < 0, G outside [1, 65536], V outside [1, 2^24], more than 2^40 heads in all,
- * overlapping strides, misaligned pointers), CHAM_E_BAD_TYPE, CHAM_E_WORKSPACE.  R = 0 is no error.
+ * overlapping strides, misaligned pointers, an output or the workspace that crosses another argument), CHAM_E_BAD_TYPE,
+ * CHAM_E_WORKSPACE.  R = 0 is no error.
  */
 int32_t cham_policy_logp(const void *logits, int32_t type, int64_t R, int32_t G, int32_t V, int64_t ld_r, int64_t ld_g,
                          const void *actions, int32_t action_type, int64_t first_action, const float *weights,
@@ -420,7 +421,8 @@ typedef struct cham_policy_coef {
  *           what is left out; other memory between strides is left as it was).  NULL: forward only.  It may be the
  *           logits themselves (same pointer and strides: in place); otherwise their ranges of addresses must not cross
  *   grad_values DEVICE float [R] or NULL
- * No other output shares memory with an input or another output.
+ * No other output, nor the workspace, shares memory with an input or another output (CHAM_E_BAD_DIM; what lies between the strides of
+ * logits or gradients is not looked at).
  * The gradient of a minimum or maximum is that of the unclipped side where both are equal.  A term whose coefficient is
  * 0 adds nothing to the total or the gradients, whatever its value.  Exponentials are taken in fp32, those of a ratio and a
  * divergence with the range of a double; differences, products and sums per decision and over decisions in double.
@@ -442,18 +444,19 @@ int64_t cham_gae_workspace_bytes(int64_t B, int64_t S);
  *   delta_t = r_t + gamma n_t V_{t+1} - V_t,  A_t = delta_t + gamma lambda n_t A_{t+1},  ret_t = A_t + V_t,
  * n_t = 0 where done_t is set and 1 elsewhere, V behind the last step = bootstrap, A behind it = 0.  A step with done_t set
  * takes nothing from behind it, not even a NaN; elsewhere what is no number goes to all earlier steps of its episode, an
- * infinity as one (also where gamma or lambda is 0).
+ * infinite advantage as one (also where lambda is 0).
  *   rewards, values DEVICE of `type` (f32, bf16, f16): step s of trajectory b at [b*ld_b + s*ld_s], any strides >= 0
  *   dones     DEVICE uint8, same addressing, or NULL (no episode ends inside)
  *   bootstrap DEVICE float [B] or NULL (zeros): value of the state behind the last step
  *   lengths   DEVICE int32 [B] or NULL (S each): steps of every trajectory, taken into [0, S]; outputs at and behind a
  *             length are left as they were
  *   advantages, returns DEVICE float at strides o_ldb, o_lds, which do not overlap; returns may be NULL; no input may share
- *             memory with an output
+ *             memory with an output, nor the workspace with either (refused where arrays without gaps cross or two begin at one
+ *             address)
  * The recurrence is evaluated in double and rounded once.  It is joined from runs of steps in an order that depends on B, S
  * and the strides alone.
  * Errors: CHAM_E_NULL, CHAM_E_BAD_DIM (B < 0, S outside [0, 2^31), B * S above 2^40, negative or overlapping strides, misaligned
- * pointers), CHAM_E_BAD_TYPE, CHAM_E_BAD_COEF (gamma or lambda outside [0, 1]), CHAM_E_WORKSPACE.
+ * pointers, shared memory), CHAM_E_BAD_TYPE, CHAM_E_BAD_COEF (gamma or lambda outside [0, 1]), CHAM_E_WORKSPACE.
  */
 int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_t r_ldb, int64_t r_lds,
                  const void *values, int64_t v_ldb, int64_t v_lds, const uint8_t *dones, int64_t d_ldb, int64_t d_lds,

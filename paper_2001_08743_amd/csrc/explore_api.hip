@@ -68,6 +68,26 @@ int32_t check_policy(PolicyArgs &a, const void *logits, int32_t type, int64_t R,
     return CHAM_OK;
 }
 
+// Addresses of a dense argument; empty without one.
+struct Span {
+    uintptr_t lo, hi;
+};
+Span span(const void *p, int64_t bytes)
+{
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    return p && bytes > 0 ? Span{at, at + (uintptr_t)bytes} : Span{0, 0};
+}
+bool crosses(const Span &a, const Span &b) { return a.lo < b.hi && b.lo < a.hi; }
+// Whether one of the first n_out spans, which are written, crosses another span.
+template <int N>
+bool shared(const Span (&spans)[N], int n_out)
+{
+    for (int i = 0; i < n_out; ++i)
+        for (int j = i + 1; j < N; ++j)
+            if (crosses(spans[i], spans[j])) return true;
+    return false;
+}
+
 bool factor(double x) { return x >= 0.0 && x <= 1.7976931348623157e308; }       // not NaN, not infinite
 
 }  // namespace
@@ -93,7 +113,11 @@ int32_t cham_policy_logp(const void *logits, int32_t type, int64_t R, int32_t G,
     if (e != CHAM_OK) return e;
     if (R == 0) return CHAM_OK;
     if (!logp) return CHAM_E_NULL;
-    if (!workspace_ok(workspace, workspace_bytes, plan_policy(R, G, V, type, false).bytes)) return CHAM_E_WORKSPACE;
+    const int64_t need = plan_policy(R, G, V, type, false).bytes, heads = R * G;
+    if (!workspace_ok(workspace, workspace_bytes, need)) return CHAM_E_WORKSPACE;
+    const Span spans[] = {span(logp, 4 * R), span(entropy, 4 * R), span(workspace, need), span(weights, 4 * R), span(actions, heads * a.abytes),
+                          span(logits, extent == heads * V ? extent * type_bytes(type) : 0)};
+    if (shared(spans, 3)) return CHAM_E_BAD_DIM;
     const hipError_t h = launch_policy(a, type, workspace, reinterpret_cast<hipStream_t>(stream));
     return h == hipSuccess ? CHAM_OK : hip_fail(h);
 }
@@ -130,7 +154,20 @@ int32_t cham_policy_loss(const void *logits, int32_t type, int64_t R, int32_t G,
         a.gld_r = R > 1 ? gld_r : 0;
         a.gld_g = G > 1 ? gld_g : 0;
     }
-    if (!workspace_ok(workspace, workspace_bytes, plan_policy(R, G, V, type, grad_logits != nullptr).bytes)) return CHAM_E_WORKSPACE;
+    const int64_t need = plan_policy(R, G, V, type, grad_logits != nullptr).bytes, heads = R * G;
+    if (!workspace_ok(workspace, workspace_bytes, need)) return CHAM_E_WORKSPACE;
+    if (R > 0) {
+        // logits and their gradients have been compared above; here where they are dense, as others may stand between their strides
+        const bool gdense = grad_logits && grad_logits != logits && g_extent == heads * V;
+        const Span spans[] = {span(terms, 4 * CHAM_TERMS), span(logp, 4 * R), span(entropy, 4 * R), span(grad_values, 4 * R), span(workspace, need),
+                              span(weights, 4 * R), span(old_logp, 4 * R), span(advantages, 4 * R), span(ref_logp, 4 * R), span(values, 4 * R),
+                              span(old_values, 4 * R), span(returns, 4 * R), span(actions, heads * a.abytes),
+                              span(logits, extent == heads * V ? extent * type_bytes(type) : 0)};
+        if (shared(spans, 5)) return CHAM_E_BAD_DIM;
+        const Span grad = span(gdense || (grad_logits == logits && extent == heads * V) ? grad_logits : nullptr, heads * V * type_bytes(type));
+        for (int i = 0; i < 13; ++i)
+            if (crosses(grad, spans[i])) return CHAM_E_BAD_DIM;
+    }
     a.w_all = R > 0 ? 1.0 / (double)R : 0.0;
     // without decisions the pointer only says that this is a loss
     a.old_logp = old_logp ? old_logp : terms;
@@ -184,12 +221,25 @@ int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_
             eb > ((int64_t)1 << 59))
             return CHAM_E_BAD_DIM;
     }
-    int64_t extent;
+    int64_t extent;                                        // items from the first to behind the last output
     if (!apart(B, o_ldb, S, o_lds, 1, extent)) return CHAM_E_BAD_DIM;
     if (!aligned(rewards, type_bytes(type)) || !aligned(values, type_bytes(type)) || !aligned(bootstrap, 4) || !aligned(lengths, 4) ||
         !aligned(advantages, 4) || !aligned(returns, 4))
         return CHAM_E_BAD_DIM;
     if (!workspace_ok(workspace, workspace_bytes, need)) return CHAM_E_WORKSPACE;
+    // Arrays without gaps are compared as a whole; others may lie between each other's strides and are compared where they begin.
+    const int64_t n = B * S;
+    const auto array = [&](const void *p, int64_t ldb, int64_t lds, int bytes) {
+        return span(p, bytes * ((B - 1) * ldb + (S - 1) * lds + 1 == n ? n : 1));
+    };
+    const bool dense_out = extent == n;
+    const Span out[] = {span(advantages, dense_out ? 4 * n : 4), span(returns, dense_out ? 4 * n : 4), span(workspace, need)};
+    const Span in[] = {array(rewards, r_ldb, r_lds, type_bytes(type)), array(values, v_ldb, v_lds, type_bytes(type)), array(dones, d_ldb, d_lds, 1),
+                       span(bootstrap, 4 * B), span(lengths, 4 * B)};
+    if (shared(out, 3)) return CHAM_E_BAD_DIM;
+    for (const Span &o : out)
+        for (const Span &i : in)
+            if (crosses(o, i)) return CHAM_E_BAD_DIM;
     // side by side: of rewards, values and outputs the same step of all trajectories stands closer together than the steps of one
     const bool dense = r_lds == 1 && v_lds == 1 && (!dones || d_lds == 1) && o_lds == 1;
     const int layout = B >= 8 && r_ldb < r_lds && v_ldb < v_lds && o_ldb < o_lds ? kGaeSide : dense ? kGaeDense : kGaeStrided;
