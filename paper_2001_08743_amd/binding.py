@@ -749,9 +749,9 @@ class GradList:
             codes.append(_type_of(t, _FLOAT_TYPES, f"tensor {i}"))
         self.ptrs = (C.c_void_p * max(n, 1))(*[t.data_ptr() for t in self.tensors])
         self.numels = (C.c_int64 * max(n, 1))(*[t.numel() for t in self.tensors])
-        filled = [p for p, m in zip(self.ptrs, self.numels) if m > 0]
-        if len(set(filled)) != len(filled):
-            raise ChamError("a tensor stands twice in the list")
+        spans = sorted((p, p + m * (4 if code == TYPE_F32 else 2)) for p, m, code in zip(self.ptrs, self.numels, codes) if m > 0)
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ChamError("tensors of the list share memory")
         self.types = (C.c_int32 * max(n, 1))(*codes)
         self.sizes = bytes(self.numels) + bytes(self.types)
         self.workspace_bytes = _check(load().cham_grad_workspace_bytes(self.numels, self.types, n))
