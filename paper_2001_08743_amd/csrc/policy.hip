@@ -1010,9 +1010,17 @@ __global__ void __launch_bounds__(kThreads) policy_grad_kernel(const PolicyArgs 
 
 constexpr int kGroup = 16;
 constexpr int kGroupHeads = 256;                 // at most: what LDS holds of the four decisions of a workgroup
-// us a loss, in three steps / so: bf16 4096 x 24 x 100 97 / 32, x 256 91 / 38, x 1000 123 / 144 (fp32 85 / 33, 87 / 55, 236 / 273); fp32 1024 x 24 x 100
-// 30 / 19, 256 x 24 x 100 17 / 19, 512 x 250 x 70 110 / 158: few decisions leave the chip empty.
-constexpr int kGroupChoices = 512, kGroupRows = 1024;
+constexpr int kGroupChoices = 512, kGroupRows = 256;
+// Decisions from which this is faster than three steps.  A wave walks its decision's heads four at a time, each in so many pieces a lane, whatever the
+// number of decisions (up to 4096 on the chip), and three steps spread heads over the chip: eight decisions for every piece and head of up to 64.
+// us a loss, in three steps / so: bf16 4096 x 24 x 70 98 / 30, x 150 102 / 40, x 500 101 / 62, x 1000 123 / 144; 1024 x 24 x 150 34 / 23, x 500 37 / 40; 1024 x 128 x 70
+// 124 / 72, x 500 127 / 184; 2048 x 128 x 500 270 / 304; 512 x 250 x 70 124 / 132, x 500 127 / 339; 256 x 2 x 70 15 / 10; fp32 1024 x 128 x 500 2.5
+// times as long so, 4096 x 24 x 500 1.2 times (the rows of all waves leave the caches before their second read), 4096 x 250 x 70 0.4 times.
+inline int64_t group_rows(int G, int V, int type)
+{
+    const int64_t pieces = (V / (16 / type_bytes(type)) + kGroup - 1) / kGroup, rows = 8 * pieces * (G < 64 ? G : 64);
+    return rows > kGroupRows ? rows : kGroupRows;
+}
 
 // Maximum and sum over sixteen lanes, in each of them, by rotations.
 __device__ __forceinline__ Soft soft_group(Soft v)
@@ -1288,7 +1296,7 @@ PolicyPlan plan_policy(int64_t R, int G, int V, int type, bool grad)
         p.bytes = (int64_t)kRowBlocks * kPolicySums * 8;
         return p;
     }
-    if (G > 1 && G <= kGroupHeads && V <= kGroupChoices && R >= kGroupRows) {
+    if (G > 1 && G <= kGroupHeads && V <= kGroupChoices && R >= group_rows(G, V, type)) {
         p.group = kGroup;
         p.bytes = (int64_t)kTileBlocks * kPolicySums * 8;
         return p;
