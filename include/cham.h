@@ -375,7 +375,8 @@ int64_t cham_policy_workspace_bytes(int64_t R, int32_t G, int32_t V, int32_t typ
  *   entropy[r] = sum_g ( - sum_v p[r,g,v] log p[r,g,v] )
  *   logits  DEVICE [R][G][V] of `type` (f32, bf16, f16), aligned to its items
  *   actions DEVICE [R][G] dense, of action_type (i8, i32, i64)
- *   weights DEVICE float [R] or NULL: a decision of weight 0 is left out: nothing of it is read, its outputs are 0
+ *   weights DEVICE float [R] or NULL: a decision of weight 0 is left out: its outputs are 0, whatever its
+ *           logits, actions and other inputs hold (they may be read)
  *   logp, entropy DEVICE float [R]; entropy may be NULL
  * A masked choice has the logit -inf (or its type's lowest value): probability 0, nothing added to the entropy.  A head
  * whose choices are all -inf, or whose action is below first_action (a padded knob), is left out of its decision; a

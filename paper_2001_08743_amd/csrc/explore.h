@@ -29,14 +29,14 @@ struct PolicyArgs {
     int64_t gld_r, gld_g;
     float *grad_values;
     double *sums;                  // [blocks][kPolicySums] partial sums of the terms
-    float *part;                   // [R*G][splits][4] maximum, sum of exponentials, sum of exponential x exponent
-    float4 *head;                  // [R*G] maximum, log of the sum, entropy, class of the action (int bits; negative: left out)
+    float *part;                   // [R*G][splits][4] maximum, sum of exponentials, sum of exponential x exponent, logit of the action (in its part)
+    float4 *head;                  // [R*G] maximum, sum of exponentials, entropy, choice of the action (int bits; negative: left out)
     float2 *dec;                   // [R] derivative by the log-probability, factor of the entropy's derivative
 };
 
 // How a call is run; a function of its sizes and type alone, so that the workspace can be asked for ahead of it.
 struct PolicyPlan {
-    int lanes;                     // up to four choices a head: lanes of a decision; 0 elsewhere
+    int lanes;                     // up to 64 choices a head: lanes of a decision, four heads each up to four choices; 0 elsewhere
     int tile;                      // few choices a head: decisions of a tile; 0 elsewhere
     int row, threads;              // one head: 16-byte pieces of a row that each of so many threads holds; 0 elsewhere
     int group;                     // several heads of many decisions: lanes that take one at a time; 0 elsewhere
