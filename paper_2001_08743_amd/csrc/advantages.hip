@@ -356,7 +356,7 @@ GaePlan plan_gae(int64_t B, int64_t S, int layout)
     GaePlan p;
     // Dense rows: a wave up to 512 steps, four to 2048, eight beyond so that two rows share a compute unit (512 x up to 8192 16 us; sixteen
     // waves, one row, 18).  Few long rows: chunks of four waves' tiles (3 x 200003 12 us; of sixteen waves' 16), until there are two workgroups
-    // for every compute unit.
+    // for every compute unit.  A plan knows of no device, as the workspace is asked for ahead of it: it is made for the 256 units of the whole card.
     p.threads = layout == kGaeSide ? kSideThreads
                 : layout == kGaeStrided ? 256
                 : S <= 64 * kSteps ? 64

@@ -16,6 +16,7 @@ static dim3_t g_grid, g_block;
 static size_t g_shared;
 static void *g_stream;
 static int launches, fails;
+static uint32_t first_grid;                /* of a call */
 static const char *what = "";
 
 int __hipPushCallConfiguration(dim3_t grid, dim3_t block, size_t shared, void *stream)
@@ -37,7 +38,7 @@ int __hipPopCallConfiguration(dim3_t *grid, dim3_t *block, size_t *shared, void 
 int hipLaunchKernel(const void *kernel, dim3_t grid, dim3_t block, void **args, size_t shared, void *stream)
 {
     (void)kernel, (void)args, (void)shared, (void)stream;
-    ++launches;
+    if (launches++ == 0) first_grid = grid.x;
     const int ok = grid.x > 0 && block.x > 0 && block.x <= 1024 && (uint64_t)grid.x * block.x < (1ull << 32) && grid.y == 1 && grid.z == 1 &&
                    block.y == 1 && block.z == 1;
     if (!ok) {
@@ -47,6 +48,18 @@ int hipLaunchKernel(const void *kernel, dim3_t grid, dim3_t block, void **args, 
     return ok ? 0 : 9;                     /* hipErrorInvalidConfiguration */
 }
 int hipGetLastError(void) { return 0; }
+static int cus = 256;
+int hipGetDevice(int *device)
+{
+    *device = 0;
+    return 0;
+}
+int hipDeviceGetAttribute(int *value, int attribute, int device)
+{
+    (void)attribute, (void)device;         /* the library asks for the compute units alone */
+    *value = cus;
+    return 0;
+}
 
 static void *const kAt = (void *)(uintptr_t)0x100000;
 #define AT(i) ((void *)((uintptr_t)(i) << 53))       /* arguments far apart */
@@ -113,6 +126,25 @@ int main(void)
                 snprintf(text, sizeof text, "advantages %lld x %lld, strides %lld %lld", (long long)B, (long long)S, (long long)b, (long long)s);
                 expect(cham_gae(0, B, S, AT(1), b, s, AT(2), b, s, AT(3), b, s, AT(4), AT(5), 0.9, 0.9, AT(6), AT(7), b, s, AT(8), bytes, 0), 1);
             }
+    /* rows that stay in a workgroup: as many workgroups as the device's units hold */
+    const int32_t rows_of[] = {1000, 8191, 32768, 131072};
+    for (int i = 0; i < 4; ++i) {
+        uint32_t grids[3];
+        const int units[3] = {256, 32, 512};
+        for (int k = 0; k < 3; ++k) {
+            cus = units[k];
+            const int64_t bytes = cham_policy_workspace_bytes(100000, 1, rows_of[i], CHAM_TYPE_BF16, 1);
+            snprintf(text, sizeof text, "rows of %d on %d units", rows_of[i], cus);
+            expect(cham_policy_loss(AT(1), CHAM_TYPE_BF16, 100000, 1, rows_of[i], rows_of[i], 0, AT(2), CHAM_TYPE_I32, 0, 0, AT(3), AT(4), AT(5), AT(6), AT(7), AT(8),
+                                    &c, AT(9), AT(10), AT(11), AT(12), rows_of[i], 0, AT(13), AT(14), bytes, 0), 2);
+            grids[k] = first_grid;
+        }
+        if (grids[0] != 8 * grids[1] || grids[2] != grids[0] || (int64_t)grids[0] * 40 > cham_policy_workspace_bytes(100000, 1, rows_of[i], CHAM_TYPE_BF16, 1)) {
+            fprintf(stderr, "explore_launch_check: rows of %d: %u, %u, %u workgroups\n", rows_of[i], grids[0], grids[1], grids[2]);
+            ++fails;
+        }
+    }
+    cus = 256;
     if (fails) return 1;
     printf("explore_launch_check ok\n");
     return 0;

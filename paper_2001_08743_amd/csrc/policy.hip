@@ -11,6 +11,7 @@
 // blur, and their constants spill registers (us a loss, so / with them: 64000 x 24 x 3 20.5 / 21.7, 16384 x 1000 29.6 / 38.0, bf16 4096 x 131072 433 / 485,
 // 4096 x 24 x 100 31.8 / 32.3).
 #include "cham_device.h"
+#include "cham_internal.h"
 #include "explore.h"
 #include "explore_items.h"
 
@@ -1115,8 +1116,8 @@ __global__ void __launch_bounds__(kThreads) policy_group_kernel(const PolicyArgs
 
 constexpr int kJoinBlocks = 1024;
 constexpr int kTileBlocks = 1024;               // what is on the chip at a time
-constexpr int kUnits = 256;                     // compute units
-constexpr int kRowBlocks = 6 * kUnits;
+constexpr int kUnits = 256;                     // compute units of the whole card: what a plan, which knows of no device, is made for
+constexpr int kRowBlocks = 6 * kUnits;          // workgroups at most that stay on the device's own units
 constexpr int kWaveChunk = 2048;                // choices of a part that a wave takes
 // Decisions that one workgroup joins, a wave each; with gradients of one head, beside the gradient's workgroups (us a loss, three launches / two: fp32 1 x 50021
 // 12.7 / 9.1, 9 x 50021 14.0 / 12.2, 16 x 131072 15.5 / 15.5, 32 x 131072 18.0 / 23.7).
@@ -1229,7 +1230,11 @@ hipError_t launch_typed(PolicyArgs &a, const PolicyPlan &p, hipStream_t s)
     if (p.row) {
         const int rows = p.threads < kThreads ? kThreads / p.threads : 1;
         const int64_t groups = (a.R + rows - 1) / rows;
-        const int64_t resident = (int64_t)kUnits * (row_waves(p.row) * 4 / (p.threads < kThreads ? kThreads / 64 : p.threads / 64));
+        int cus = 0;
+        const hipError_t e = compute_units(cus);
+        if (e != hipSuccess) return e;
+        if (cus > kUnits) cus = kUnits;
+        const int64_t resident = (int64_t)cus * (row_waves(p.row) * 4 / (p.threads < kThreads ? kThreads / 64 : p.threads / 64));
         // Log-probabilities alone: a workgroup for every long row, which the hardware spreads better than a fixed share (us, bf16, share / each:
         // 4096 x 32768 52.2 / 46.5, 16384 x 16384 113 / 101; by waves 6001 x 8191 22.4 / 23.8).  With gradients, whose stores the next row's
         // loads run under, and a loss's sums, a share (4096 x 131072 440 / 474, 16384 x 1000 22.7 / 26.5).
