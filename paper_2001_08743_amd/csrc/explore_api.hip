@@ -230,7 +230,7 @@ int32_t cham_gae(int32_t type, int64_t B, int64_t S, const void *rewards, int64_
     // Arrays without gaps are compared as a whole; others may lie between each other's strides and are compared where they begin.
     const int64_t n = B * S;
     const auto array = [&](const void *p, int64_t ldb, int64_t lds, int bytes) {
-        return span(p, bytes * ((B - 1) * ldb + (S - 1) * lds + 1 == n ? n : 1));
+        return p ? span(p, bytes * ((B - 1) * ldb + (S - 1) * lds + 1 == n ? n : 1)) : Span{0, 0};       // strides of nothing are not looked at
     };
     const bool dense_out = extent == n;
     const Span out[] = {span(advantages, dense_out ? 4 * n : 4), span(returns, dense_out ? 4 * n : 4), span(workspace, need)};

@@ -67,3 +67,8 @@ def test_gae(lib, out, other, strides):
     if strides[1] != 2 and other not in ("bootstrap", "lengths", "ws"):
         p[out] = p[other] + 256                           # behind its beginning: arrays without gaps
         assert call() == DIM
+
+
+def test_gae_without_dones_does_not_look_at_their_strides(lib):
+    far = (1 << 63) - 1
+    assert lib.cham_gae(0, 3, 4, A, 4, 1, 2 * A, 4, 1, None, far, far, None, None, 0.9, 0.9, 3 * A, 3 * A, 4, 1, None, 0, None) == DIM
