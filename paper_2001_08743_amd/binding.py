@@ -734,7 +734,8 @@ def cham_gae(rewards, values, gamma: float, lam: float, dones=None, bootstrap=No
 
 class GradList:
     """Addresses, sizes and types of a list of dense tensors on one device, for programs that clip the same tensors in every
-    step.  It keeps the tensors alive; a tensor whose storage is replaced needs a new list."""
+    step.  It keeps the tensors alive; a tensor whose storage is replaced needs a new list (gradients that are set to None between steps
+    are new tensors in the next)."""
 
     def __init__(self, tensors):
         _torch()

@@ -6,7 +6,7 @@
 // and every thread walks its steps once more with the advantage behind them known: one read of everything, one write.  In
 // double: the sum over a long trajectory keeps its small terms.
 // Bound by latency: a workgroup's loads, its join (shuffles and a barrier) and its stores follow each other (bf16 512 x 8192 ragged
-// 11 us, 2.2 TB/s; fp32 128 x 500 step by step 8.5 us).  Few long trajectories are cut into chunks of their own workgroups and read twice.
+// 11 us, 2.2 TB/s; fp32 128 x 500 step by step 8.9 us).  Few long trajectories are cut into chunks of their own workgroups and read twice.
 #include "cham_device.h"
 #include "explore.h"
 #include "explore_items.h"

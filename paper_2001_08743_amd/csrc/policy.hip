@@ -28,7 +28,7 @@ __device__ __forceinline__ float exp2_fast(float z) { return __builtin_amdgcn_ex
 
 // Exponents are taken to the base 2: z = (x - m) log2 e.  The difference comes first, rounded relative to itself, so that no result depends on
 // where a head's logits lie.  (x log2 e - m log2 e in one fused operation saves an instruction but carries the rounding of m log2 e, half a
-// step of a number that may be far from 0, into every exponential: three equal logits of -1e9 were 2^18 apart from their sum.)
+// step of a number that may be far from 0, into every exponential: the sum over equal logits of -1e9 was off by 2^18.)
 __device__ __forceinline__ float exponent(float x, float m) { return (x - m) * kLog2e; }
 
 // Running maximum and sums of a head: of 2^z and of z 2^z.
@@ -403,7 +403,7 @@ __device__ __forceinline__ float2 head_of(const PolicyArgs &a, Soft &v, float xa
 // A lane holds HEADS consecutive heads of up to VP choices in registers (four heads of up to four choices, one of up to 64); as many lanes as
 // that takes side by side are a decision, and a wave takes as many decisions as fit (24 heads of 3: six lanes, ten
 // decisions).  Nothing goes through LDS and no wave waits for another.  Choices from V to VP are masked ones.
-// fp32 64000 x 24 x 3 with gradients 18.7 us, of which the vector instructions are 8 and 40 MB of memory 8: the chain of loads, exponentials,
+// fp32 64000 x 24 x 3 with gradients 18.6 us, of which the vector instructions are 8 and 40 MB of memory 8: the chain of loads, exponentials,
 // shuffles and the decision in double, twice per wave.  The tile kernel below took 24 us, more than 1024 workgroups 21.
 // V = VP is known at compile time up to four, where a lane's heads are one run of items.
 template <typename T>
@@ -1133,6 +1133,7 @@ constexpr int kJoinFew = 16;
 // Beyond 4096 pieces log-probabilities alone take a row in parts, which a workgroup reads without holding it (bf16 4096 x 131072,
 // row / parts, 245 / 194 us, fp32 1024 x 50021 40 / 36; at 4096 pieces, 2048 x 32768, 26 / 28), and gradients do so for few rows:
 // the row is read twice, but by many workgroups: 9 x 131072 bf16 24 / 15, 64 26 / 23, 128 30 / 31; fp32 32 x 50021 19 / 17, 128 23 / 26.
+// (All pairs: before the exponents' difference became an instruction of its own, which adds 0 to 5 % to either side.)
 constexpr int kWideRow = 4096;
 constexpr int kFewRows = 1024, kVeryFewRows = 256;
 constexpr unsigned kMostBlocks = 1u << 20;
