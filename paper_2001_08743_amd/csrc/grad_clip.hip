@@ -151,45 +151,40 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double *parts
     if (threadIdx.x == 0) *norm = v;
 }
 
-// The factor, and what is multiplied: in fp32, or, by a factor that fp32 has no normal number for, in double.
-struct Factor {
-    double wide;
-    float f;
-    bool far;
-};
-
 template <typename T>
-__device__ __forceinline__ void scale_piece(typename T::item *q, int i, const uint4 &raw, const Factor &f)
+__device__ __forceinline__ void scale_piece(typename T::item *q, int i, const uint4 &raw, float f)
 {
     float x[T::kVec];
     T::unpack(raw, x);
-    if (f.far) {
 #pragma unroll
-        for (int j = 0; j < T::kVec; ++j) x[j] = (float)((double)x[j] * f.wide);
-    } else {
-#pragma unroll
-        for (int j = 0; j < T::kVec; ++j) x[j] *= f.f;
-    }
+    for (int j = 0; j < T::kVec; ++j) x[j] *= f;
     const uint4 v = T::pack(x);
     const typename T::words w = {v.x, v.y, v.z, v.w};
     __builtin_nontemporal_store(w, reinterpret_cast<typename T::words *>(q + i * T::kVec));
 }
+// Products by the factor f: in fp32, or, where that has no normal number for it, in double, an item at a time (the code of pieces for both cost
+// small lists 3 %, a choice in every piece large ones 1 %).
 template <typename T>
-__device__ __forceinline__ void chunk_scale(const void *from, void *to, int n, const Factor &f)
+__device__ __forceinline__ void chunk_scale(const void *from, void *to, const Chunk &c, double f, bool far)
 {
-    const typename T::item *p = static_cast<const typename T::item *>(from);
-    typename T::item *q = static_cast<typename T::item *>(to);
-    const int tid = threadIdx.x, n_vec = n / T::kVec, at = n_vec * T::kVec + tid;
+    const typename T::item *p = static_cast<const typename T::item *>(from) + c.at;
+    typename T::item *q = static_cast<typename T::item *>(to) + c.at;
+    const int tid = threadIdx.x, n_vec = c.n / T::kVec, at = n_vec * T::kVec + tid;
+    if (far) {
+#pragma unroll 1
+        for (int i = tid; i < c.n; i += kThreads) q[i] = T::put((float)((double)T::get(p[i]) * f));
+        return;
+    }
     uint4 held[kPieces];
 #pragma unroll
     for (int k = 0; k < kPieces; ++k)
         if (tid + k * kThreads < n_vec) held[k] = piece<T>(p, tid + k * kThreads);
     typename T::item last{};
-    if (at < n) last = p[at];
+    if (at < c.n) last = p[at];
 #pragma unroll
     for (int k = 0; k < kPieces; ++k)
-        if (tid + k * kThreads < n_vec) scale_piece<T>(q, tid + k * kThreads, held[k], f);
-    if (at < n) q[at] = T::put(f.far ? (float)((double)T::get(last) * f.wide) : T::get(last) * f.f);
+        if (tid + k * kThreads < n_vec) scale_piece<T>(q, tid + k * kThreads, held[k], (float)f);
+    if (at < c.n) q[at] = T::put(T::get(last) * (float)f);
 }
 
 // parts: the sums of squares of this call (block 0 of the first launch notes the norm); null: *norm is given.
@@ -204,8 +199,8 @@ __global__ void __launch_bounds__(kThreads, 8) grad_clip_kernel(const Tensors<MO
         v = *norm;
     }
     const bool whole = v + 1e-6 <= max_norm;
-    const double wide = whole ? 1.0 : max_norm / (v + 1e-6);
-    const Factor f{wide, (float)wide, wide < 0x1p-126 && wide > 0.0};
+    const double f = whole ? 1.0 : max_norm / (v + 1e-6);
+    const bool far = f < 0x1p-126 && f > 0.0;
     int lo, hi;
     share_of(t, lo, hi);
     // from the last chunk to the first: what the sum of squares has read last is still in cache
@@ -213,9 +208,9 @@ __global__ void __launch_bounds__(kThreads, 8) grad_clip_kernel(const Tensors<MO
         while (c < t.first[i]) --i;
         if (whole && t.from[i] == t.to[i]) continue;
         const Chunk k = chunk_of(t, i, c);
-        if (k.type == 0) chunk_scale<F32>(static_cast<const float *>(t.from[i]) + k.at, static_cast<float *>(t.to[i]) + k.at, k.n, f);
-        else if (k.type == 1) chunk_scale<BF16>(static_cast<const __bf16 *>(t.from[i]) + k.at, static_cast<__bf16 *>(t.to[i]) + k.at, k.n, f);
-        else chunk_scale<F16>(static_cast<const _Float16 *>(t.from[i]) + k.at, static_cast<_Float16 *>(t.to[i]) + k.at, k.n, f);
+        if (k.type == 0) chunk_scale<F32>(t.from[i], t.to[i], k, f, far);
+        else if (k.type == 1) chunk_scale<BF16>(t.from[i], t.to[i], k, f, far);
+        else chunk_scale<F16>(t.from[i], t.to[i], k, f, far);
     }
 }
 
